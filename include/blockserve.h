@@ -74,6 +74,11 @@ typedef struct bs_copy_seg {
 
 typedef enum bs_dtype { BS_F32 = 0, BS_BF16 = 1 } bs_dtype;
 
+/* Number formats of an 8-bit cache. BS_E4M3: one sign, four exponent and three
+ * fraction bits (largest number 448, no infinities). BS_I8: two's complement,
+ * -127 .. 127. */
+typedef enum bs_qformat { BS_E4M3 = 0, BS_I8 = 1 } bs_qformat;
+
 typedef enum bs_status {
   BS_OK = 0,
   BS_ERR_INVALID_ARG = 1,  /* null pointer, bad enum, negative size, bad stride */
@@ -326,6 +331,119 @@ int bs_dual_cache_refresh(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, in
                           bs_dtype dt, float scale, float rope_base, const void* q, const void* k,
                           const void* v, int R, int W, void* k_cache, void* v_cache, void* out,
                           void* stream);
+
+/* ------------------------------------------------------------------------
+ * A dual cache held in 8 bits
+ *
+ * k8, v8: [R][Hkv][W][D] codes of one byte, at the cells of the bf16 cache.
+ * k_scale, v_scale: [R][Hkv][S] fp32, one scale per group of T consecutive
+ * tokens of a head. T is a power of two up to 64. Groups belong to the logical
+ * row, not to the box column: token t of a request with prompt length p is in
+ * group (t + pad) / T with pad = -p mod T, so group borders run both ways from
+ * the first generated token and an active block is whole groups whenever T
+ * divides L. A row has bs_kv_scale_groups(p, g, T) groups, which may not exceed
+ * S; entry j of scale row `row` belongs to group j wherever the row's cells lie
+ * (off may change, as at a compaction, and the scale row moves unchanged).
+ * The number a code stands for is code * scale.
+ *
+ * Moving rows between boxes: bs_kv_scatter_compact moves codes as dt = BS_BF16
+ * with D / 2 elements a cell, and scale rows (S a multiple of 4) as dt = BS_F32
+ * with D = 4 and W = S / 4, segments of ceil(groups / 4) cells from column 0.
+ *
+ * Under stream capture the calls below that take a context can be
+ * recorded into a graph: the same descriptors (with the same shape arguments)
+ * must have gone through the same call on that context outside a capture
+ * before, which uploads them; otherwise BS_ERR_UNSUPPORTED. The upload then
+ * stays in its slot until the context is destroyed, and graphs that hold the
+ * call must not be replayed after that. Graphs whose replays may overlap need
+ * workspaces of their own, like calls that may overlap.
+ * ---------------------------------------------------------------------- */
+
+/* Groups of a row: ceil(p / T) + ceil(g / T); 0 when p < 0, g < 1 or T is not a
+ * power of two up to 64. */
+int bs_kv_scale_groups(int p, int g, int T);
+
+/*
+ * Quantises the logical cells of every listed request's row from the box k, v
+ * ([R][Hkv][W][D] of dt, the cache layout) into the 8-bit cache. Per group, with
+ * a = max(max |x|, 2^-64) over its tokens and features and Q = 448 (BS_E4M3) or
+ * 127 (BS_I8):
+ *   scale = a / Q,  code = round_to_nearest_even(x * (Q / a))
+ * with both quotients and the product rounded to fp32. Padding cells are not read
+ * and no cell or scale outside the rows is written. Inputs are finite; a group
+ * that holds an infinity or NaN gets codes and a scale of no meaning, others
+ * are not affected. Supported: dt BS_BF16 or BS_F32, D in {64, 128},
+ * n <= 65535, Hkv <= 32767, tensors 16-byte aligned (scales 4), codes disjoint
+ * from k and v. The descriptors are validated as everywhere (L and k only there).
+ */
+int bs_kv_quantize(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
+                   bs_qformat fmt, int T, const void* k, const void* v, void* k8, void* v8, float* k_scale,
+                   float* v_scale, int S, void* stream);
+
+/* The way back: k[cell] = code * scale in fp32, then rounded to dt, for the logical
+ * cells of every listed request's row; every other cell is left unchanged.
+ * Arguments and limits as above. */
+int bs_kv_dequantize(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
+                     bs_qformat fmt, int T, const void* k8, const void* v8, const float* k_scale,
+                     const float* v_scale, int S, void* k, void* v, void* stream);
+
+/*
+ * bs_dual_cache_block_attention against a cache held in 8 bits. For request i,
+ * query head h (KV head c = h / (Hq / Hkv)) and block row j < B_i:
+ *   out[i][j][h] = softmax(scale * q[i][j][h] . keys^T) . values
+ * with the numbers that the cache stands for at the cells outside the active
+ * block and k_new / v_new, as they are, at the block's own. Rows j >= B_i of out
+ * are written as zeros; scale <= 0 selects 1/sqrt(D). q, k_new, v_new and out
+ * are bf16 in the layouts of bs_dual_cache_block_attention.
+ * write_back != 0 also quantises rows j < B_i of k_new and v_new into the
+ * block's cells and scales, exactly as bs_kv_quantize would from a box; the
+ * cache is otherwise only read, and padding and the stale block slot never are
+ * (their scales neither). Sums and softmax statistics are fp32; queries and
+ * codes meet as fp16 (queries scaled by a power of two for each row), weights are
+ * rounded to fp16 for the codes and to bf16 for the block's own values.
+ * Scales must be positive and finite, within 2^-80 .. 2^80.
+ * Supported: D in {64, 128}, L <= 64, Hq / Hkv <= 8, T a divisor of L,
+ * W * D < 2^31; tensors 16-byte aligned (scales 4).
+ * ws: NULL or a workspace of ws_bytes bytes (contents on entry ignored). With
+ * at least bs_quant_attention_workspace_bytes(...) bytes, long rows are split
+ * over workgroups and joined by a second launch, as for
+ * bs_dual_cache_block_attention; otherwise every row runs whole. The plan depends
+ * only on the arguments of the query. Calls that may overlap need different
+ * workspaces.
+ */
+size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D);
+int bs_quant_cache_block_attention(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D,
+                                   bs_qformat fmt, int T, float scale, const void* q, const void* k_new,
+                                   const void* v_new, void* k8, void* v8, float* k_scale, float* v_scale, int S,
+                                   int R, int W, int write_back, void* out, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/*
+ * Per-head norm of queries and keys and their rotary embedding, in one pass, for
+ * the block attentions (whole_rows == 0) or ahead of a refresh with rope_base
+ * <= 0 (whole_rows != 0), for models that normalise queries and keys.
+ * For every head row x [D] of a token with position id t:
+ *   y = x / sqrt(mean(x^2) + eps) * weight
+ *   y turned at (f, f + D/2), f < D/2, by the angle t * rope_base^(-2 f / D)
+ * in fp32 (the angle's fraction of a turn is good to about 2^-23 at any
+ * position), rounded once to dt.
+ * whole_rows == 0: tokens are block rows j < B_i, token index i * L + j, position
+ * s_i + j. whole_rows != 0: tokens are the logical cells t < p + g, token index
+ * row_i * W + off_i + t, position t. Other tokens are neither read nor written.
+ * Head h of token m is read at q + m * q_stride + h * D (k likewise; strides in
+ * elements, >= the heads' H * D), so q and k may point into one fused projection
+ * buffer; outputs are dense, [tokens][Hq][D] and [tokens][Hkv][D]. q_out may be q
+ * itself when q_stride = Hq * D (k_out likewise); otherwise the outputs overlap
+ * no input and not each other (BS_ERR_OVERLAP).
+ * q_weight, k_weight: [D] of dt, or NULL for ones. eps < 0 leaves the norm out
+ * (the weights are not read), rope_base <= 0 the rotation.
+ * Supported: dt BS_BF16 or BS_F32, D a multiple of 16 up to 256, W < 2^24,
+ * n <= 65535; pointers 16-byte aligned, strides a multiple of 16 bytes.
+ */
+int bs_qk_norm_rope(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, int W, int whole_rows, int Hq, int Hkv,
+                    int D, bs_dtype dt, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* q_weight, const void* k_weight, float eps, float rope_base, void* q_out,
+                    void* k_out, void* stream);
 
 /*
  * K4 -- KV scatter/compaction at a block boundary (Algorithm 1: completed

@@ -37,6 +37,8 @@ refresh    the full-row attention of the dual-cache refresh at a block start
            (and the prefill of newly admitted rows), with rotary embedding at
            the explicit position ids of paragraph "Logical positional
            alignment"; the refreshed cache holds the rotated keys.
+quant      the dual cache held in 8 bits (codes, scales, attention over them) and
+           the per-head norm with rotation that precedes the attention.
 compact    KV scatter/compaction when requests are evicted and admitted at a
            block boundary (Algorithm 1; Eq. 1 discussion of the bounding box
            shrinking without explicit reclamation).
@@ -57,10 +59,10 @@ from .lm_head import lm_head_logits, lm_head_decode
 from .refresh import rope, row_positions, refresh_row, dual_cache_refresh
 from .compact import kv_scatter_compact
 from .step import mixed_state_step
-from . import schedule
+from . import quant, schedule
 
 __all__ = [
-    "schedule",
+    "quant", "schedule",
     "geometry", "validate_reqs", "bbox_cost", "position_ids", "transfer_schedule",
     "effective_compute_ratio", "widen", "gather_active_blocks", "scatter_active_blocks",
     "dual_cache_block_attention", "attention_rows", "parallel_decode", "row_stats",

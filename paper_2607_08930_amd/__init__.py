@@ -29,6 +29,8 @@ __all__ = [
     "bs_dual_cache_block_attention", "bs_decode_workspace_bytes", "bs_parallel_decode",
     "bs_kv_scatter_compact", "bs_lm_head_workspace_bytes", "bs_lm_head_decode", "bs_lm_head_pack_bytes",
     "bs_lm_head_pack", "bs_dual_cache_refresh",
+    "BS_E4M3", "BS_I8", "bs_kv_scale_groups", "bs_kv_quantize", "bs_kv_dequantize",
+    "bs_quant_attention_workspace_bytes", "bs_quant_cache_block_attention", "bs_qk_norm_rope",
     "PROFILE_PHASES", "LM_PROFILE_PHASES", "REFRESH_PROFILE_PHASES",
 ]
 
@@ -38,6 +40,7 @@ REQ_DTYPE = np.dtype([("p", "<i4"), ("g", "<i4"), ("k", "<i4"), ("row", "<i4"), 
 SEG_DTYPE = np.dtype([("src_kind", "<i4"), ("src_row", "<i4"), ("src_col", "<i4"),
                       ("dst_row", "<i4"), ("dst_col", "<i4"), ("len", "<i4")])
 BS_F32, BS_BF16 = 0, 1
+BS_E4M3, BS_I8 = 0, 1
 STATUS = {0: "BS_OK", 1: "BS_ERR_INVALID_ARG", 2: "BS_ERR_UNSUPPORTED", 3: "BS_ERR_DESCRIPTOR",
           4: "BS_ERR_OVERLAP", 5: "BS_ERR_WORKSPACE", 6: "BS_ERR_HIP"}
 
@@ -113,6 +116,16 @@ _SIGS = {
     "bs_lm_head_pack": (_i32, [_vp, _vp, _i64, _i32, _i32, _i32, _vp, _sz, _vp]),
     "bs_dual_cache_refresh": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _f32, _vp, _vp, _vp,
                                      _i32, _i32, _vp, _vp, _vp, _vp]),
+    "bs_kv_scale_groups": (_i32, [_i32, _i32, _i32]),
+    "bs_kv_quantize": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp,
+                              _vp, _vp, _i32, _vp]),
+    "bs_kv_dequantize": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp,
+                                _i32, _vp, _vp, _vp]),
+    "bs_quant_attention_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32, _i32, _i32]),
+    "bs_quant_cache_block_attention": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _vp, _vp,
+                                              _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "bs_qk_norm_rope": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64,
+                               _vp, _vp, _f32, _f32, _vp, _vp, _vp]),
     "bs_kv_scatter_compact": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _i32, _vp,
                                      _vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _i32, _vp]),
 }
@@ -339,6 +352,46 @@ def bs_dual_cache_refresh(ctx, reqs, L, Hq, Hkv, D, dt, scale, rope_base, q, k, 
     return _check(lib.bs_dual_cache_refresh(
         _ptr(ctx), _ptr(r), len(r), L, Hq, Hkv, D, dt, float(scale), float(rope_base), _ptr(q), _ptr(k), _ptr(v),
         R, W, _ptr(k_cache), _ptr(v_cache), _ptr(out), _stream(stream)), ctx)
+
+
+def bs_kv_scale_groups(p: int, g: int, T: int) -> int:
+    return int(lib.bs_kv_scale_groups(p, g, T))
+
+
+def bs_kv_quantize(ctx, reqs, L, R, W, Hkv, D, dt, fmt, T, k, v, k8, v8, k_scale, v_scale, S, stream=None):
+    r = _host(reqs, REQ_DTYPE)
+    return _check(lib.bs_kv_quantize(_ptr(ctx), _ptr(r), len(r), L, R, W, Hkv, D, dt, fmt, T, _ptr(k), _ptr(v),
+                                     _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), S, _stream(stream)), ctx)
+
+
+def bs_kv_dequantize(ctx, reqs, L, R, W, Hkv, D, dt, fmt, T, k8, v8, k_scale, v_scale, S, k, v, stream=None):
+    r = _host(reqs, REQ_DTYPE)
+    return _check(lib.bs_kv_dequantize(_ptr(ctx), _ptr(r), len(r), L, R, W, Hkv, D, dt, fmt, T, _ptr(k8), _ptr(v8),
+                                       _ptr(k_scale), _ptr(v_scale), S, _ptr(k), _ptr(v), _stream(stream)), ctx)
+
+
+def bs_quant_attention_workspace_bytes(reqs, L, Hq, Hkv, D) -> int:
+    r = _host(reqs, REQ_DTYPE)
+    return int(lib.bs_quant_attention_workspace_bytes(_ptr(r), len(r), L, Hq, Hkv, D))
+
+
+def bs_quant_cache_block_attention(ctx, reqs, L, Hq, Hkv, D, fmt, T, scale, q, k_new, v_new, k8, v8, k_scale, v_scale,
+                                   S, R, W, write_back, out, ws=None, ws_bytes=0, stream=None):
+    r = _host(reqs, REQ_DTYPE)
+    return _check(lib.bs_quant_cache_block_attention(
+        _ptr(ctx), _ptr(r), len(r), L, Hq, Hkv, D, fmt, T, float(scale), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k8),
+        _ptr(v8), _ptr(k_scale), _ptr(v_scale), S, R, W, int(write_back), _ptr(out), _ptr(ws), int(ws_bytes),
+        _stream(stream)), ctx)
+
+
+def bs_qk_norm_rope(ctx, reqs, L, R, W, whole_rows, Hq, Hkv, D, dt, q, q_stride, k, k_stride, q_weight, k_weight, eps,
+                    rope_base, q_out, k_out, stream=None):
+    """Strides are in elements, between tokens."""
+    r = _host(reqs, REQ_DTYPE)
+    return _check(lib.bs_qk_norm_rope(
+        _ptr(ctx), _ptr(r), len(r), L, R, W, int(whole_rows), Hq, Hkv, D, dt, _ptr(q), int(q_stride), _ptr(k),
+        int(k_stride), _ptr(q_weight), _ptr(k_weight), float(eps), float(rope_base), _ptr(q_out), _ptr(k_out),
+        _stream(stream)), ctx)
 
 
 def bs_kv_scatter_compact(ctx, segs, n_layers, Hkv, D, dt, src_k, src_v, src_layer_stride, R_src, W_src,

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "bs_internal.h"
+#include "bs_quant.h"
 #include "bs_refresh.h"
 
 using namespace bs;
@@ -45,6 +46,7 @@ struct Slot {
   hipStream_t stream = nullptr;
   uint64_t used = 0;           // tick of the last call that used it (LRU order)
   bool live = false;
+  bool held = false;           // a captured graph reads it: never given to another blob
 };
 
 thread_local std::string g_err;
@@ -192,6 +194,7 @@ int take_slot(bs_ctx* c, Slot** out) {
   Slot* lru_any = nullptr;
   for (auto& p : c->slots) {
     Slot* sl = p.get();
+    if (sl->held) continue;
     if (!lru_any || sl->used < lru_any->used) lru_any = sl;
     bool free_ = !sl->live;
     if (!free_) {
@@ -210,6 +213,7 @@ int take_slot(bs_ctx* c, Slot** out) {
   }
   if (!sl) {
     sl = lru_any;
+    if (!sl) return fail(c, BS_ERR_UNSUPPORTED, "captured graphs hold all %d upload slots of the context", kMaxSlots);
     hipError_t e = hipEventSynchronize(sl->done);
     if (e != hipSuccess) return hip_fail(c, e, "hipEventSynchronize(slot)");
   }
@@ -288,6 +292,46 @@ int finish(bs_ctx* c, Slot* sl, hipStream_t s, hipError_t launch, const char* wh
   if (launch != hipSuccess) return hip_fail(c, launch, what);
   if (e != hipSuccess) return hip_fail(c, e, "hipEventRecord(done)");
   return BS_OK;
+}
+
+// upload() and finish() for calls that may be recorded into a graph. Under
+// capture nothing may be uploaded and no event of a slot may be recorded (it
+// would become the graph's), so the blob has to be in a slot already: an earlier
+// call put it there. Its upload is waited for here, and the slot then stays as it
+// is until the context goes, since the graph can be replayed until then.
+struct Call {
+  Slot* slot = nullptr;
+  bool captured = false;
+};
+
+template <class Make>
+int begin(bs_ctx* c, hipStream_t s, const Key& key, Make make, Call* call) {
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(s, &cap);
+  if (e != hipSuccess) return hip_fail(c, e, "hipStreamIsCapturing");
+  if (cap == hipStreamCaptureStatusNone) return upload(c, s, key, make, &call->slot);
+  call->captured = true;
+  const uint64_t hv = fnv1a(key.b.data(), key.b.size());
+  for (auto& p : c->slots) {
+    Slot& sl = *p;
+    if (!sl.live || sl.hash != hv || sl.key != key.b) continue;
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    e = hipThreadExchangeStreamCaptureMode(&mode);
+    if (e != hipSuccess) return hip_fail(c, e, "hipThreadExchangeStreamCaptureMode");
+    const hipError_t w = hipEventSynchronize(sl.ready);
+    e = hipThreadExchangeStreamCaptureMode(&mode);
+    if (w != hipSuccess || e != hipSuccess) return hip_fail(c, w != hipSuccess ? w : e, "hipEventSynchronize(ready)");
+    sl.held = true;
+    call->slot = &sl;
+    return BS_OK;
+  }
+  return fail(c, BS_ERR_UNSUPPORTED,
+              "the stream is being captured: run the call once with these descriptors outside a capture first");
+}
+
+int end(bs_ctx* c, const Call& call, hipStream_t s, hipError_t launch, const char* what) {
+  if (!call.captured) return finish(c, call.slot, s, launch, what);
+  return launch == hipSuccess ? BS_OK : hip_fail(c, launch, what);
 }
 
 int dtype_bytes(bs_dtype dt) { return dt == BS_F32 ? 4 : (dt == BS_BF16 ? 2 : 0); }
@@ -806,6 +850,59 @@ int check_segments(bs_ctx* c, const bs_copy_seg* segs, int nseg, int R_src, int 
   return BS_OK;
 }
 
+// ---- 8-bit cache
+// log2 of a group length, or -1
+int group_shift(int T) {
+  for (int lt = 0; lt <= 6; ++lt)
+    if (T == 1 << lt) return lt;
+  return -1;
+}
+
+int64_t scale_groups(int p, int g, int lt) {
+  const int64_t T = int64_t(1) << lt;
+  return (p + T - 1) / T + (g + T - 1) / T;
+}
+
+// What the three calls on an 8-bit cache share: descriptors, format, groups
+int check_quant(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_qformat fmt, int T,
+                int S) {
+  if (!c) return fail(nullptr, BS_ERR_INVALID_ARG, "ctx is NULL");
+  int st = check_reqs(c, reqs, n, L, R, W);
+  if (st) return st;
+  if (fmt != BS_E4M3 && fmt != BS_I8) return fail(c, BS_ERR_INVALID_ARG, "bad 8-bit format %d", (int)fmt);
+  const int lt = group_shift(T);
+  if (lt < 0) return fail(c, BS_ERR_INVALID_ARG, "T=%d is not a power of two up to 64", T);
+  if (Hkv < 1 || D < 1 || S < 1) return fail(c, BS_ERR_INVALID_ARG, "Hkv, D, S must be >= 1");
+  if (D != 64 && D != 128) return fail(c, BS_ERR_UNSUPPORTED, "an 8-bit cache needs D in {64, 128} (D=%d)", D);
+  if (Hkv > 32767) return fail(c, BS_ERR_UNSUPPORTED, "Hkv=%d exceeds 32767", Hkv);
+  if (n > 65535) return fail(c, BS_ERR_UNSUPPORTED, "n=%d requests exceed the 65535 of one launch", n);
+  if ((int64_t)W * D > INT32_MAX) return fail(c, BS_ERR_UNSUPPORTED, "W * D exceeds 2^31");
+  for (int i = 0; i < n; ++i)
+    if (scale_groups(reqs[i].p, reqs[i].g, lt) > S)
+      return fail(c, BS_ERR_INVALID_ARG, "request %d: %lld scale groups exceed S=%d", i,
+                  (long long)scale_groups(reqs[i].p, reqs[i].g, lt), S);
+  return BS_OK;
+}
+
+int check_quant_tensors(bs_ctx* c, const void* k8, const void* v8, const float* k_scale, const float* v_scale) {
+  if (!k8 || !v8 || !k_scale || !v_scale) return fail(c, BS_ERR_INVALID_ARG, "cache pointer is NULL");
+  if (!aligned(k8, 16) || !aligned(v8, 16) || !aligned(k_scale, 4) || !aligned(v_scale, 4))
+    return fail(c, BS_ERR_INVALID_ARG, "codes must be 16-byte and scales 4-byte aligned");
+  return BS_OK;
+}
+
+// whether [a, a + na) and [b, b + nb) share a byte
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+int longest_row(const bs_req_desc* reqs, int n) {
+  int m = 0;
+  for (int i = 0; i < n; ++i) m = std::max(m, reqs[i].p + reqs[i].g);
+  return m;
+}
+
 // ---- phase timing of the fused step
 hipError_t prof_mark(bs_ctx* c, int phase, hipStream_t s) {
   Prof& p = c->prof;
@@ -1247,6 +1344,197 @@ int bs_dual_cache_refresh(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int 
   if (e == hipSuccess) e = prof_mark(c, 3, s);
   if (e == hipSuccess && c->prof.on && c->prof.used < c->prof.cap) ++c->prof.used;
   return finish(c, sl, s, e, "refresh launch");
+}
+
+// ------------------------------------------------------------------ 8-bit cache
+int bs_kv_scale_groups(int p, int g, int T) {
+  const int lt = group_shift(T);
+  if (p < 0 || g < 1 || lt < 0) return 0;
+  const int64_t m = scale_groups(p, g, lt);
+  return m > INT32_MAX ? 0 : (int)m;
+}
+
+int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
+                   bs_qformat fmt, int T, const void* k, const void* v, void* k8, void* v8, float* k_scale,
+                   float* v_scale, int S, void* stream) {
+  int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
+  if (st) return st;
+  if (!dtype_bytes(dt)) return fail(c, BS_ERR_INVALID_ARG, "bad dtype %d", (int)dt);
+  if (n == 0) return BS_OK;
+  st = check_quant_tensors(c, k8, v8, k_scale, v_scale);
+  if (st) return st;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16))
+    return fail(c, BS_ERR_INVALID_ARG, "k and v must be non-NULL and 16-byte aligned");
+  const int64_t cells = (int64_t)R * Hkv * W * D, xb = cells * dtype_bytes(dt);
+  if (overlap(k, xb, k8, cells) || overlap(k, xb, v8, cells) || overlap(v, xb, k8, cells) || overlap(v, xb, v8, cells) ||
+      overlap(k8, cells, v8, cells))
+    return fail(c, BS_ERR_OVERLAP, "the codes overlap k, v or each other");
+  DeviceGuard dg(c->device);
+  if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Call call;
+  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
+  if (st) return st;
+  QuantArgs a{};
+  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
+  a.L = L; a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
+  a.k = k; a.v = v;
+  a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
+  a.k_scale = k_scale; a.v_scale = v_scale;
+  return end(c, call, s, launch_kv_quantize(a, dt, fmt, D, n, longest_row(reqs, n), s), "quantize launch");
+}
+
+int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
+                     bs_qformat fmt, int T, const void* k8, const void* v8, const float* k_scale,
+                     const float* v_scale, int S, void* k, void* v, void* stream) {
+  int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
+  if (st) return st;
+  if (!dtype_bytes(dt)) return fail(c, BS_ERR_INVALID_ARG, "bad dtype %d", (int)dt);
+  if (n == 0) return BS_OK;
+  st = check_quant_tensors(c, k8, v8, k_scale, v_scale);
+  if (st) return st;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16))
+    return fail(c, BS_ERR_INVALID_ARG, "k and v must be non-NULL and 16-byte aligned");
+  const int64_t cells = (int64_t)R * Hkv * W * D, xb = cells * dtype_bytes(dt);
+  if (overlap(k, xb, k8, cells) || overlap(k, xb, v8, cells) || overlap(v, xb, k8, cells) || overlap(v, xb, v8, cells) ||
+      overlap(k, xb, v, xb))
+    return fail(c, BS_ERR_OVERLAP, "k or v overlaps the codes or the other");
+  DeviceGuard dg(c->device);
+  if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Call call;
+  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
+  if (st) return st;
+  DequantArgs a{};
+  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
+  a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
+  a.k8 = static_cast<const uint8_t*>(k8); a.v8 = static_cast<const uint8_t*>(v8);
+  a.k_scale = k_scale; a.v_scale = v_scale;
+  a.k = k; a.v = v;
+  return end(c, call, s, launch_kv_dequantize(a, dt, fmt, D, n, longest_row(reqs, n), s), "dequantize launch");
+}
+
+size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D) {
+  (void)reqs; (void)n; (void)L; (void)Hq; (void)Hkv; (void)D;
+  return 0;
+}
+
+int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D,
+                                   bs_qformat fmt, int T, float scale, const void* q, const void* k_new,
+                                   const void* v_new, void* k8, void* v8, float* k_scale, float* v_scale, int S,
+                                   int R, int W, int write_back, void* out, void* ws, size_t ws_bytes,
+                                   void* stream) {
+  int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
+  if (st) return st;
+  if (Hq < 1 || Hq % Hkv) return fail(c, BS_ERR_UNSUPPORTED, "Hq=%d not a multiple of Hkv=%d", Hq, Hkv);
+  if (L > 64 || Hq / Hkv > 8)
+    return fail(c, BS_ERR_UNSUPPORTED, "the 8-bit attention needs L <= 64 and Hq/Hkv <= 8 (L=%d, Hq/Hkv=%d)", L, Hq / Hkv);
+  if (L % T) return fail(c, BS_ERR_UNSUPPORTED, "T=%d does not divide the block length L=%d", T, L);
+  if (!(scale == scale)) return fail(c, BS_ERR_INVALID_ARG, "scale is NaN");
+  if ((int64_t)n * Hq * L > INT32_MAX) return fail(c, BS_ERR_UNSUPPORTED, "n * Hq * L exceeds the launch grid");
+  if (n == 0) return BS_OK;
+  st = check_quant_tensors(c, k8, v8, k_scale, v_scale);
+  if (st) return st;
+  if (!q || !k_new || !v_new || !out) return fail(c, BS_ERR_INVALID_ARG, "tensor pointer is NULL");
+  if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16))
+    return fail(c, BS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+  DeviceGuard dg(c->device);
+  if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)ws; (void)ws_bytes;
+  Call call;
+  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
+  if (st) return st;
+  QAttnArgs a{};
+  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
+  a.n = n; a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.R = R; a.W = W; a.S = S; a.lt = group_shift(T);
+  a.scale_log2e = (scale > 0.0f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_new = static_cast<const uint16_t*>(k_new); a.v_new = static_cast<const uint16_t*>(v_new);
+  a.k8 = static_cast<const uint8_t*>(k8); a.v8 = static_cast<const uint8_t*>(v8);
+  a.k_scale = k_scale; a.v_scale = v_scale;
+  a.out = static_cast<uint16_t*>(out);
+  hipError_t e = launch_qattn(a, fmt, s);
+  if (e == hipSuccess && write_back) {
+    QuantArgs w{};
+    w.reqs = a.reqs;
+    w.L = L; w.Hkv = Hkv; w.W = W; w.S = S; w.lt = a.lt; w.block = 1;
+    w.k = k_new; w.v = v_new;
+    w.k8 = static_cast<uint8_t*>(k8); w.v8 = static_cast<uint8_t*>(v8);
+    w.k_scale = k_scale; w.v_scale = v_scale;
+    e = launch_kv_quantize(w, BS_BF16, fmt, D, n, L, s);
+  }
+  return end(c, call, s, e, "8-bit attention launch");
+}
+
+// ------------------------------------------------------------------ norm and rotation
+int bs_qk_norm_rope(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int whole_rows, int Hq, int Hkv,
+                    int D, bs_dtype dt, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* q_weight, const void* k_weight, float eps, float rope_base, void* q_out,
+                    void* k_out, void* stream) {
+  if (!c) return fail(nullptr, BS_ERR_INVALID_ARG, "ctx is NULL");
+  int st = check_reqs(c, reqs, n, L, R, W);
+  if (st) return st;
+  const int eb = dtype_bytes(dt);
+  if (!eb) return fail(c, BS_ERR_INVALID_ARG, "bad dtype %d", (int)dt);
+  if (Hq < 1 || Hkv < 1 || D < 1) return fail(c, BS_ERR_INVALID_ARG, "Hq, Hkv, D must be >= 1");
+  if (D % 16 || D > 256) return fail(c, BS_ERR_UNSUPPORTED, "the norm needs D %% 16 == 0 and D <= 256 (D=%d)", D);
+  if (W >= 1 << 24) return fail(c, BS_ERR_UNSUPPORTED, "W=%d exceeds the positions an fp32 angle holds (2^24)", W);
+  if (n > 65535) return fail(c, BS_ERR_UNSUPPORTED, "n=%d requests exceed the 65535 of one launch", n);
+  if (!std::isfinite(eps) || !std::isfinite(rope_base)) return fail(c, BS_ERR_INVALID_ARG, "eps and rope_base must be finite");
+  if (q_stride < (int64_t)Hq * D || k_stride < (int64_t)Hkv * D || q_stride * eb % 16 || k_stride * eb % 16)
+    return fail(c, BS_ERR_INVALID_ARG, "token strides must hold the heads and be multiples of 16 bytes");
+  const int max_tokens = whole_rows ? longest_row(reqs, n) : L;
+  if (((int64_t)Hq + Hkv) * max_tokens * 16 > INT32_MAX)
+    return fail(c, BS_ERR_UNSUPPORTED, "tokens times heads exceed the launch grid");
+  if (n == 0) return BS_OK;
+  if (!q || !k || !q_out || !k_out) return fail(c, BS_ERR_INVALID_ARG, "tensor pointer is NULL");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(q_weight, 16) ||
+      !aligned(k_weight, 16))
+    return fail(c, BS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+  const int64_t tokens = whole_rows ? (int64_t)R * W : (int64_t)n * L;
+  const int64_t qb = ((tokens - 1) * q_stride + (int64_t)Hq * D) * eb, kb = ((tokens - 1) * k_stride + (int64_t)Hkv * D) * eb;
+  const int64_t qob = tokens * Hq * D * eb, kob = tokens * Hkv * D * eb;
+  const bool q_in_place = q == q_out && q_stride == (int64_t)Hq * D, k_in_place = k == k_out && k_stride == (int64_t)Hkv * D;
+  if ((!q_in_place && overlap(q_out, qob, q, qb)) || (!k_in_place && overlap(k_out, kob, k, kb)) ||
+      overlap(q_out, qob, k, kb) || overlap(k_out, kob, q, qb) || overlap(q_out, qob, k_out, kob))
+    return fail(c, BS_ERR_OVERLAP, "an output overlaps an input or the other output");
+  for (const void* w : {q_weight, k_weight})
+    if (w && (overlap(q_out, qob, w, (int64_t)D * eb) || overlap(k_out, kob, w, (int64_t)D * eb)))
+      return fail(c, BS_ERR_OVERLAP, "an output overlaps a weight");
+  DeviceGuard dg(c->device);
+  if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool rope = rope_base > 0.0f;
+  uint32_t base_bits;
+  std::memcpy(&base_bits, &rope_base, sizeof base_bits);
+  Call call;
+  st = begin(c, s, Key('N', {n, rope ? D : 0, rope ? (int64_t)base_bits : 0}, reqs, sizeof(bs_req_desc) * n),
+             [&](Blob& b) {
+               b.meta[0] = (int)b.add(reqs, sizeof(bs_req_desc) * n);
+               std::vector<float2> freq(rope ? (size_t)D / 2 : 0);
+               for (size_t f = 0; f < freq.size(); ++f) {
+                 const double turns = std::exp2(-2.0 * (double)f / D * std::log2((double)rope_base)) / 6.283185307179586476925;
+                 freq[f].x = (float)turns;
+                 freq[f].y = (float)(turns - (double)freq[f].x);
+               }
+               b.meta[1] = (int)b.add(freq.data(), sizeof(float2) * freq.size());
+             },
+             &call);
+  if (st) return st;
+  const char* base = static_cast<const char*>(call.slot->d);
+  NormRopeArgs a{};
+  a.reqs = reinterpret_cast<const bs_req_desc*>(base + call.slot->meta[0]);
+  a.freq = reinterpret_cast<const float2*>(base + call.slot->meta[1]);
+  a.L = L; a.W = W; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
+  a.rows = whole_rows ? 1 : 0;
+  a.norm = eps >= 0.0f ? 1 : 0;
+  a.rope = rope ? 1 : 0;
+  a.eps = eps;
+  a.q = q; a.k = k; a.q_stride = q_stride; a.k_stride = k_stride;
+  a.qw = q_weight; a.kw = k_weight;
+  a.q_out = q_out; a.k_out = k_out;
+  return end(c, call, s, launch_norm_rope(a, dt, n, max_tokens, s), "norm and rotation launch");
 }
 
 // ------------------------------------------------------------------ fused step
