@@ -67,9 +67,35 @@ struct DequantArgs {
 hipError_t launch_kv_dequantize(const DequantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_len,
                                 hipStream_t s);
 
+// Attention work item: the row tiles of one (request, KV head) that one workgroup
+// serves, against the cached keys [v0, v1) of its piece in virtual keys (below) and,
+// where `fresh` is set, the block's own keys.
+// Virtual keys count the cached keys without the active block from pad = -p mod 64:
+// v < s + pad is cell v - pad, v >= s + pad is cell v - pad + B; nv ends them. Groups
+// of T <= 64 tokens and 64-key tiles then share borders. v0 and v1 are multiples of
+// 64, but for v1 = nv of the last piece.
+struct QItem {
+  int32_t req, kvh, rt0;     // request, KV head, first row tile
+  int32_t row, off, s, B;
+  int32_t pad, nv, v0, v1;
+  int32_t part;              // partial slot of a split row, or -1
+  int32_t fresh;
+  int32_t pad_[3];
+};
+
+struct QMerge {
+  int32_t req, kvh, rt0, B, part0, nparts, pad_[2];
+};
+
+constexpr int kQTile = 64;   // virtual keys per planning unit
+constexpr int kQRowTiles = 8;   // most 32-row tiles (waves) per workgroup
+
 struct QAttnArgs {
-  const bs_req_desc* reqs;
-  int n, L, Hq, Hkv, D, G, R, W, S, lt;
+  const QItem* items;
+  const QMerge* merges;
+  int n_items, n_merge;
+  int RTW;                   // row tiles per workgroup
+  int L, Hq, Hkv, D, G, W, S, lt;
   float scale_log2e;
   const uint16_t* q;         // [n][L][Hq][D] bf16
   const uint16_t* k_new;     // [n][L][Hkv][D]
@@ -79,6 +105,7 @@ struct QAttnArgs {
   const float* k_scale;
   const float* v_scale;
   uint16_t* out;             // [n][L][Hq][D]
+  float* parts;              // part_wave_floats(D) per wave of a partial slot
 };
 hipError_t launch_qattn(const QAttnArgs& a, bs_qformat fmt, hipStream_t s);
 

@@ -897,6 +897,85 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// ---- 8-bit attention plan
+// Row tiles of 32 query rows (j G + h') per KV head and per workgroup: up to
+// kQRowTiles waves a workgroup, the tiles of a head spread evenly over as few of
+// them as that takes.
+struct QRows {
+  int tiles, groups, per;   // row tiles of a head, workgroups, row tiles per workgroup
+};
+
+QRows qattn_rows(int L, int Hq, int Hkv) {
+  QRows q;
+  q.tiles = (Hq / Hkv * L + 31) / 32;
+  q.groups = (q.tiles + kQRowTiles - 1) / kQRowTiles;
+  q.per = (q.tiles + q.groups - 1) / q.groups;
+  return q;
+}
+
+QItem qattn_row(const bs_req_desc& r, int i, int L) {
+  const Geo geo = geo_of(r, L);
+  QItem it{};
+  it.req = i; it.row = r.row; it.off = r.off; it.s = geo.s; it.B = geo.B;
+  it.pad = group_pad(r.p, 6);
+  it.nv = geo.len > geo.B ? it.pad + geo.len - geo.B : 0;
+  it.v1 = it.nv;
+  it.part = -1;
+  it.fresh = 1;
+  return it;
+}
+
+PlanShape qattn_shape(const QRows& q) { return q.per == 1 ? PlanShape{kMhaWaves, 2.0, kMergePerPartWave} : PlanShape{1, 1.3, kMergePerPartShared}; }
+
+int qattn_tiles(const QItem& it) { return std::max(1, (it.nv + kQTile - 1) / kQTile); }
+
+// Longest piece in tiles, or 0 to leave every row whole
+int qattn_cap(const bs_req_desc* reqs, int n, int L, int Hkv, const QRows& q) {
+  std::vector<Run> runs((size_t)n);
+  for (int i = 0; i < n; ++i) runs[i] = Run{qattn_tiles(qattn_row(reqs[i], i, L)), Hkv * q.groups};
+  return split_cap(runs, qattn_shape(q));
+}
+
+size_t qattn_part_bytes(int parts, const QRows& q, int D) {
+  return (size_t)parts * q.per * part_wave_floats(D) * sizeof(float);
+}
+
+// meta = {items, item count, merges, merge count, partial slots, descriptors}
+void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, bool split) {
+  const QRows q = qattn_rows(L, Hq, Hkv);
+  const int cap = split ? qattn_cap(reqs, n, L, Hkv, q) : 0;
+  std::vector<QItem> items;
+  std::vector<QMerge> merges;
+  int parts = 0;
+  for (int i = 0; i < n; ++i) {
+    const QItem row = qattn_row(reqs[i], i, L);
+    const int nt = qattn_tiles(row), np = cap > 0 && nt > cap ? (nt + cap - 1) / cap : 1;
+    for (int h = 0; h < Hkv; ++h)
+      for (int gr = 0; gr < q.groups; ++gr) {
+        QItem it = row;
+        it.kvh = h;
+        it.rt0 = gr * q.per;
+        if (np > 1) merges.push_back(QMerge{i, h, it.rt0, it.B, parts, np, {0, 0}});
+        for (int k = 0; k < np; ++k) {
+          if (np > 1) {
+            it.v0 = k * cap * kQTile;
+            it.v1 = std::min(row.nv, (k + 1) * cap * kQTile);
+            it.part = parts++;
+            it.fresh = k == 0;
+          }
+          items.push_back(it);
+        }
+      }
+  }
+  std::stable_sort(items.begin(), items.end(), [](const QItem& x, const QItem& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
+  blob.meta[0] = (int)blob.add(items.data(), sizeof(QItem) * items.size());
+  blob.meta[1] = (int)items.size();
+  blob.meta[2] = (int)blob.add(merges.data(), sizeof(QMerge) * merges.size());
+  blob.meta[3] = (int)merges.size();
+  blob.meta[4] = parts;
+  blob.meta[5] = (int)blob.add(reqs, sizeof(bs_req_desc) * n);
+}
+
 int longest_row(const bs_req_desc* reqs, int n) {
   int m = 0;
   for (int i = 0; i < n; ++i) m = std::max(m, reqs[i].p + reqs[i].g);
@@ -1415,8 +1494,16 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
 }
 
 size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D) {
-  (void)reqs; (void)n; (void)L; (void)Hq; (void)Hkv; (void)D;
-  return 0;
+  if (!reqs || n <= 0 || L < 1 || L > 64 || Hkv < 1 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 8 || (D != 64 && D != 128)) return 0;
+  const QRows q = qattn_rows(L, Hq, Hkv);
+  const int cap = qattn_cap(reqs, n, L, Hkv, q);
+  int parts = 0;
+  if (cap > 0)
+    for (int i = 0; i < n; ++i) {
+      const int nt = qattn_tiles(qattn_row(reqs[i], i, L));
+      if (nt > cap) parts += (nt + cap - 1) / cap * Hkv * q.groups;
+    }
+  return qattn_part_bytes(parts, q, D);
 }
 
 int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D,
@@ -1438,16 +1525,28 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   if (!q || !k_new || !v_new || !out) return fail(c, BS_ERR_INVALID_ARG, "tensor pointer is NULL");
   if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16))
     return fail(c, BS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+  if (ws && !aligned(ws, 16)) return fail(c, BS_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
   DeviceGuard dg(c->device);
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  (void)ws; (void)ws_bytes;
+  const QRows q_rows = qattn_rows(L, Hq, Hkv);
   Call call;
-  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
-  if (st) return st;
+  for (int split = ws ? 1 : 0; split >= 0; --split) {
+    st = begin(c, s, Key('K', {n, L, Hq, Hkv, split}, reqs, sizeof(bs_req_desc) * n),
+               [&](Blob& blob) { qattn_blob(blob, reqs, n, L, Hq, Hkv, split != 0); }, &call);
+    if (st) return st;
+    if (qattn_part_bytes(call.slot->meta[4], q_rows, D) <= ws_bytes) break;
+  }
+  const char* base = static_cast<const char*>(call.slot->d);
+  const int* meta = call.slot->meta;
   QAttnArgs a{};
-  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
-  a.n = n; a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.R = R; a.W = W; a.S = S; a.lt = group_shift(T);
+  a.items = reinterpret_cast<const QItem*>(base + meta[0]);
+  a.n_items = meta[1];
+  a.merges = reinterpret_cast<const QMerge*>(base + meta[2]);
+  a.n_merge = meta[3];
+  a.parts = static_cast<float*>(ws);
+  a.RTW = q_rows.per;
+  a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.scale_log2e = (scale > 0.0f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   a.q = static_cast<const uint16_t*>(q);
   a.k_new = static_cast<const uint16_t*>(k_new); a.v_new = static_cast<const uint16_t*>(v_new);
@@ -1457,7 +1556,7 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   hipError_t e = launch_qattn(a, fmt, s);
   if (e == hipSuccess && write_back) {
     QuantArgs w{};
-    w.reqs = a.reqs;
+    w.reqs = reinterpret_cast<const bs_req_desc*>(base + meta[5]);
     w.L = L; w.Hkv = Hkv; w.W = W; w.S = S; w.lt = a.lt; w.block = 1;
     w.k = k_new; w.v = v_new;
     w.k8 = static_cast<uint8_t*>(k8); w.v8 = static_cast<uint8_t*>(v8);

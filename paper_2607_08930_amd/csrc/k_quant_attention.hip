@@ -1,92 +1,453 @@
 // Block attention against a dual cache held in 8 bits.
 //
-// As the attention over the bf16 cache, with key t of the row read as
-// code * scale of its group outside the active block, and from k_new / v_new
-// inside it. One wave per (request, query head, block row): lane t scores key t
-// of each 64-key chunk, the weights are broadcast by lane shuffles for P V.
+// As the attention over the bf16 cache (k_attention.hip), with key t of the row
+// read as code * scale of its group outside the active block, and from k_new /
+// v_new inside it.
+//
+// Row tiles. The query rows of a KV head's group are counted r = j G + h' (block
+// row j, head h' of the group), so that short blocks of grouped heads fill the 32
+// columns of an MFMA; a wave owns 32 of them, a workgroup up to eight waves that
+// share the K/V tiles.
+//
+// Virtual keys. The cached keys (prefix and suffix without the active block) are
+// counted v = pad + 0, 1, ..., pad = -p mod 64. Block borders lie at multiples
+// of T in v, and so does the seam where the block was left out, so groups of 32
+// and 64 tokens cover whole 32-key sub-tiles and their scale is one number for the
+// whole wave (UNI). Smaller groups take a scale for each key from LDS.
+//
+// Per sub-tile: S^T = K Q^T with v_mfma_f32_32x32x16_bf16 (keys on the M axis),
+// online softmax on one query column a lane, O^T += V^T P^T with the weights fed
+// straight from the accumulators. Codes become bf16 in registers, exactly (e4m3
+// has 4 significant bits, int8 7, bf16 8); a K read of 16 codes feeds two MFMAs,
+// since the order of the contraction is free, and V comes out of LDS transposed,
+// 8 keys of one feature a lane (ds_read_b64_tr_b8). The K scale is folded into the
+// exponent's factor and the V scale into its offset:
+//   p' = vs 2^(s ks c - m) = 2^(s ks c - (m - log2 vs)),
+// so neither costs an instruction per key; the row sum takes (sum p') / vs.
+// The weights are rounded to bf16, whose range holds any scale allowed; fp16 would
+// round eight times finer, but a weight times a small scale leaves its range.
+#include "bs_lds.h"
 #include "bs_quant.h"
 
 namespace bs {
 namespace {
 
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4;
+typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
+
+__device__ inline float vmax(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// 64 lanes x 4 bytes, HBM -> the 256 bytes of LDS at `lds` (wave-uniform)
+__device__ inline void dma4(uint32_t lds, const void* gptr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(gptr)
+               : "memory");
+}
+
+// eight codes as bf16
 template <int FMT>
-__global__ __launch_bounds__(256) void k_qattn(QAttnArgs a, int jblocks) {
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int jb = blockIdx.x % jblocks, rest = blockIdx.x / jblocks;
-  const int h = rest % a.Hq, i = rest / a.Hq, j = jb * 4 + w;
-  if (j >= a.L) return;
-  const bs_req_desc r = a.reqs[i];
-  const Geo geo = geo_of(r, a.L);
-  const int c = h / a.G, D = a.D, pad = group_pad(r.p, a.lt), bs = geo.s, be = geo.s + geo.B;
-  uint16_t* op = a.out + (((int64_t)i * a.L + j) * a.Hq + h) * D;
-  if (j >= geo.B) {
-    for (int d = lane; d < D; d += 64) op[d] = 0;
+__device__ inline bf16x8_t widen8(uint32_t lo, uint32_t hi) {
+  bf16x2_t x[4];
+  if constexpr (FMT == BS_E4M3) {
+    x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.0f, false);
+    x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.0f, true);
+    x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.0f, false);
+    x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.0f, true);
+  } else {
+    float y[8];
+    float (&a)[4] = *reinterpret_cast<float (*)[4]>(y);
+    float (&b)[4] = *reinterpret_cast<float (*)[4]>(y + 4);
+    decode4<FMT>(lo, a);
+    decode4<FMT>(hi, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_convertvector(qf2{y[2 * i], y[2 * i + 1]}, bf16x2_t);
+  }
+  return bf16x8_t{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+}
+
+// XOR swizzles of a row's 16-byte slots, for an LDS that serves 256 bytes a cycle.
+// Codes: a row has D / 16 slots, so 256 bytes are two rows (D = 128) or four
+// (64). K reads take one chunk of 16 consecutive rows: the row pairs (quadruples)
+// get distinct slots. V reads take chunks c and c ^ 1 of rows 0-3 and 8-11 (or 4-7
+// and 12-15): bits 0 and 2 of the pair's number go to slot bits 1 and 2.
+template <int D>
+__device__ inline int swz8(int row) {
+  if constexpr (D == 128) {
+    const int rp = row >> 1;
+    return (rp & 4) | ((rp & 1) << 1) | ((rp >> 1) & 1);
+  }
+  return (row >> 2) & 3;
+}
+// bf16 rows of the block: D / 8 slots, as in k_attention.hip
+template <int D>
+__device__ inline int swz16(int row) {
+  if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  return ((row & 3) << 1) | ((row >> 2) & 1);
+}
+
+// Tiles and ring of a workgroup of up to MAXW waves
+template <int MAXW>
+struct Shape {
+  static constexpr int KT = MAXW == 1 ? 32 : 64;              // keys per stage
+  static constexpr int NS = 4;                                // stages
+  static constexpr int NI = MAXW == 1 ? 1 : MAXW == 4 ? 2 : 4;   // waves that issue the DMA
+};
+
+template <int FMT, int D, int MAXW, bool UNI>
+__global__ __launch_bounds__(64 * MAXW, MAXW == 1 ? 1 : 2) void k_qattn(QAttnArgs a) {
+  using SH = Shape<MAXW>;
+  constexpr int KT = SH::KT, NS = SH::NS, NI = SH::NI, SPT = KT / 32;
+  constexpr int NKK = D / 16, NDT = D / 32, NC = D / 16, NCB = D / 8;
+  constexpr int TILE = KT * D, STAGE = 2 * TILE;   // bytes: K tile, then V tile
+  constexpr int RPB = 1024 / D;                    // rows per 1 KiB DMA block
+  constexpr int RPI = KT / RPB / NI;               // blocks per tensor and issuing wave
+  constexpr int PB = 2 * RPI + 1;                  // DMA instructions per stage and issuing wave
+  constexpr int SCB = 2 * KT * 4;                  // bytes of a stage's scales
+  static_assert(KT / RPB % NI == 0, "issuing waves split a tile evenly");
+  __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB];
+
+  const QItem it = a.items[blockIdx.x];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31, q16 = lane >> 4, j16 = lane & 15;
+  const int c = it.kvh, B = it.B, pad = it.pad, seam = it.s + it.pad, lt = a.lt;
+  const int v0 = it.v0 ? it.v0 : pad & ~(KT - 1), v1 = it.v1;   // virtual keys of this piece
+  const int ntiles = v1 > v0 ? (v1 - v0 + KT - 1) / KT : 0;
+  const bool issuer = w < NI;
+  const int64_t row_head = (int64_t)it.row * a.Hkv + c;
+  const uint8_t* kcb = a.k8 + (row_head * a.W + it.off) * D;
+  const uint8_t* vcb = a.v8 + (row_head * a.W + it.off) * D;
+  // group of virtual key v: groups count from the row's own pad, -p mod T
+  const int g0 = (pad - (pad & ((1 << lt) - 1))) >> lt, glen = a.L >> lt;
+  const float* ksb = a.k_scale + row_head * a.S - g0;
+  const float* vsb = a.v_scale + row_head * a.S - g0;
+  auto cell = [&](int v) { return v - pad + (v >= seam ? B : 0); };
+
+  // queries of this lane's column: row r = j G + h' of the group; feature
+  // 32 c + 16 g + 8 h + e of MFMA 2 c + h
+  const int r = (it.rt0 + w) * 32 + n, rq = min(r, a.G * B - 1), j = rq / a.G;
+  bf16x8_t qb[NKK];
+  {
+    const uint16_t* qp = a.q + (((int64_t)it.req * a.L + j) * a.Hq + c * a.G + (rq - j * a.G)) * D + 16 * g;
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) qb[kk] = __builtin_bit_cast(bf16x8_t, ld16(qp + 32 * (kk >> 1) + 8 * (kk & 1)));
+  }
+
+  const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  auto issue = [&](int u) {
+    if (!issuer) return;
+    const int slot = u % NS, vb = v0 + u * KT;
+    const uint32_t sbase = ring_lds + (uint32_t)(slot * STAGE + w * 1024);
+    const bool whole = vb >= pad && vb + KT <= it.nv && (vb + KT <= seam || vb >= seam);
+#pragma unroll
+    for (int k = 0; k < 2 * RPI; ++k) {
+      const int tensor = k / RPI, blk = k % RPI * NI;
+      const int row = (blk + w) * RPB + lane / NC, chunk = (lane % NC) ^ swz8<D>(row);
+      const uint32_t dst = sbase + (uint32_t)(tensor * TILE + blk * 1024);
+      const uint8_t* cb = tensor ? vcb : kcb;
+      if (whole) {
+        dma16_sv_once(dst, uniform64(cb + (int64_t)cell(vb) * D), (uint32_t)(row * D + chunk * 16));
+      } else {
+        // rows before the first key and past the last repeat one of them (masked later)
+        const int v = min(max(vb + row, pad), it.nv - 1);
+        dma16_once(dst, cb + (int64_t)cell(v) * D + chunk * 16);
+      }
+    }
+    // scales by key: K then V; of four issuing waves two fetch the same
+    const int key = KT == 64 ? lane : lane & 31, sel = KT == 64 ? w & 1 : lane >> 5;
+    const int v = min(max(vb + key, pad), it.nv - 1);
+    dma4(ring_lds + (uint32_t)(NS * STAGE + slot * SCB + (KT == 64 ? (w & 1) * KT * 4 : 0)),
+         (sel ? vsb : ksb) + (v >> lt) + (v >= seam ? glen : 0));
+  };
+  auto wait_stages = [&](int x) {
+    if (!issuer) return;
+    if (x <= 0)
+      wait_vm_c<0>();
+    else if (x == 1)
+      wait_vm_c<PB>();
+    else if (x == 2)
+      wait_vm_c<2 * PB>();
+    else
+      wait_vm_c<3 * PB>();
+  };
+  // every LDS read of this wave has returned, then all waves are here
+  auto barrier = [] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if constexpr (MAXW > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  f32x16_t o[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int rr = 0; rr < 16; ++rr) o[dt][rr] = 0.0f;
+  float mrun = -__builtin_inff(), mtop = -__builtin_inff(), lsum = 0.0f;
+
+  // raises the running max (log2 units) when a score exceeds it by 2^8: mx is this lane's
+  // maximum over its 16 keys, the other half-wave holds the other 16 of each column
+  auto raise = [&](float mx) {
+    if (__builtin_amdgcn_ballot_w64(mx > mtop) == 0) return;
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float mnew = fmaxf(mrun, vmax(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+    const float alpha = __builtin_amdgcn_exp2f(mrun - mnew);
+    lsum *= alpha;
+    mrun = mnew;
+    mtop = mnew + 8.0f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) o[dt][rr] *= alpha;
+  };
+  auto top16 = [](const f32x16_t& s) {
+    float m = s[0];
+#pragma unroll
+    for (int rr = 1; rr < 16; ++rr) m = vmax(m, s[rr]);
+    return m;
+  };
+  // key of accumulator register rr within the sub-tile
+  auto key_of = [&](int rr) { return 8 * (rr >> 2) + 4 * g + (rr & 3); };
+  bf16x8_t pp[2];
+  // weights 2^(s f - m) into pp; returns the sum of what the MFMA consumes
+  auto weights = [&](const f32x16_t& s, float f, float m) {
+    float t = 0.0f;
+#pragma unroll
+    for (int rr = 0; rr < 16; ++rr) pp[rr >> 3][rr & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[rr], f, -m));
+    const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      t = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{pp[i >> 2][2 * (i & 3)], pp[i >> 2][2 * (i & 3) + 1]}, one, t, false);
+    return t;
+  };
+
+  int issued = 0;
+  if (it.fresh) {
+    // the block's own rows, as bf16 in the last part of the ring
+    const int RB = (a.L + 31) / 32, FT = RB * 32 * D * 2;    // bytes per tensor
+    const int foff = NS * STAGE - 2 * FT;
+    constexpr int FR = 1024 / (2 * D);                       // rows per DMA block
+    if (issuer)
+      for (int b = w; b < 2 * FT / 1024; b += NI) {
+        const int tensor = b >= FT / 1024, bb = b - (tensor ? FT / 1024 : 0);
+        const int row = bb * FR + lane / NCB, chunk = (lane % NCB) ^ swz16<D>(row);
+        const uint16_t* src = (tensor ? a.v_new : a.k_new) +
+                              (((int64_t)it.req * a.L + min(row, B - 1)) * a.Hkv + c) * D + chunk * 8;
+        dma16(ring_lds + (uint32_t)(foff + b * 1024), src);
+      }
+    for (const int lim = min(NS - (2 * FT + STAGE - 1) / STAGE, min(NS - 1, ntiles)); issued < lim; ++issued) issue(issued);
+    wait_stages(issued);
+    barrier();
+    for (int sub = 0; sub * 32 < B; ++sub) {
+      const uint8_t* kt = ring + foff + sub * 32 * D * 2;
+      const uint8_t* vt = kt + FT;
+      f32x16_t s;
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) s[rr] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        const int chunk = 4 * (kk >> 1) + 2 * g + (kk & 1);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *reinterpret_cast<const bf16x8_t*>(kt + n * D * 2 + ((chunk ^ swz16<D>(n)) * 16)), qb[kk], s, 0, 0, 0);
+      }
+      if (sub * 32 + 32 > B) {
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr)
+          if (sub * 32 + key_of(rr) >= B) s[rr] = -__builtin_inff();
+      }
+      raise(top16(s) * a.scale_log2e);
+      lsum += weights(s, a.scale_log2e, mrun);
+#pragma unroll
+      for (int i = 0; i < 2 * NDT; ++i) {
+        const int ks = i / NDT, dt = i % NDT;
+        bf16x4_t h[2];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          const int row = 16 * ks + 8 * h2 + 4 * (q16 >> 1) + (j16 >> 2);
+          const int col = 32 * dt + 16 * (q16 & 1) + 4 * (j16 & 3);
+          h[h2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (lds_bf16x4*)(vt + row * D * 2 + (((col >> 3) ^ swz16<D>(row)) * 16) + (col & 7) * 2));
+        }
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7),
+                                                        pp[ks], o[dt], 0, 0, 0);
+      }
+    }
+    barrier();
+  }
+  for (const int lim = min(NS - 1, ntiles); issued < lim; ++issued) issue(issued);
+
+  // LDS byte offsets of this lane's K and V reads (V rows 16 apart and K rows 32
+  // apart have the same swizzle)
+  int koff[D / 32], voff[NDT];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) koff[i] = n * D + (((2 * i + g) ^ swz8<D>(n)) * 16);
+  const int vrow = (j16 >> 1 & 3) + 4 * g + (j16 >= 8 ? 8 : 0);
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+    voff[dt] = TILE + vrow * D + (((2 * dt + (q16 & 1)) ^ swz8<D>(vrow)) * 16) + 8 * (j16 & 1);
+
+  for (int u = 0; u < ntiles; ++u) {
+    wait_stages(min(NS - 2, ntiles - 1 - u));
+    barrier();
+    if (u + NS - 1 < ntiles) issue(u + NS - 1);
+    const int slot = u % NS;
+#pragma unroll
+    for (int sub = 0; sub < SPT; ++sub) {
+      const int vb = v0 + u * KT + sub * 32;
+      if (vb + 32 <= pad || vb >= v1) continue;              // wave-uniform
+      const uint8_t* tile = ring + slot * STAGE + sub * 32 * D;
+      const float* sc = reinterpret_cast<const float*>(ring + NS * STAGE + slot * SCB) + sub * 32;
+      f32x16_t s;
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) s[rr] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const v4u x = *reinterpret_cast<const v4u*>(tile + koff[i]);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[0], x[1]), qb[2 * i], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[2], x[3]), qb[2 * i + 1], s, 0, 0, 0);
+      }
+      if constexpr (!UNI) {
+#pragma unroll
+        for (int qd = 0; qd < 4; ++qd) {
+          const f32x4_t k4 = *reinterpret_cast<const f32x4_t*>(sc + 8 * qd + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * qd + e] *= k4[e] * a.scale_log2e;
+        }
+      }
+      if (vb < pad || vb + 32 > it.nv) {
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr) {
+          const int v = vb + key_of(rr);
+          if (v < pad || v >= it.nv) s[rr] = -__builtin_inff();
+        }
+      }
+      if constexpr (UNI) {
+        const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc[0]))) * a.scale_log2e;
+        const float vs = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc[KT])));
+        raise(top16(s) * f);
+        lsum = fmaf(weights(s, f, mrun - __builtin_amdgcn_logf(vs)), __builtin_amdgcn_rcpf(vs), lsum);
+      } else {
+        raise(top16(s));
+#pragma unroll
+        for (int qd = 0; qd < 4; ++qd) {
+          const f32x4_t v4 = *reinterpret_cast<const f32x4_t*>(sc + KT + 8 * qd + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int rr = 4 * qd + e;
+            const float y = __builtin_amdgcn_exp2f(s[rr] - mrun);
+            lsum += y;
+            pp[rr >> 3][rr & 7] = (__bf16)(y * v4[e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * NDT; ++i) {
+        const int ks = i / NDT, dt = i % NDT;
+        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(tile + voff[dt] + ks * 16 * D));
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]), pp[ks], o[dt], 0, 0, 0);
+      }
+    }
+  }
+
+  const float lt_ = lsum + __shfl_xor(lsum, 32, 64);
+  // lane (g, n): O^T[feature 32 dt + 8 (rr / 4) + 4 g + rr % 4][query n]
+  if (it.part >= 0) {
+    float* pw = a.parts + ((int64_t)it.part * a.RTW + w) * part_wave_floats(D);
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k)
+      *reinterpret_cast<f32x4_t*>(pw + (k * 64 + lane) * 4) =
+          f32x4_t{o[k >> 2][4 * (k & 3)], o[k >> 2][4 * (k & 3) + 1], o[k >> 2][4 * (k & 3) + 2], o[k >> 2][4 * (k & 3) + 3]};
+    pw[D / 8 * 256 + lane] = mrun;
+    pw[D / 8 * 256 + 64 + lane] = lt_;
     return;
   }
-  const uint16_t* qp = a.q + (((int64_t)i * a.L + j) * a.Hq + h) * D;
-  const int64_t cell = (((int64_t)r.row * a.Hkv + c) * a.W + r.off) * D, sc0 = ((int64_t)r.row * a.Hkv + c) * a.S;
-  const int64_t fstride = (int64_t)a.Hkv * D, fresh = ((int64_t)i * a.L * a.Hkv + c) * D;
-  float o[2] = {0.0f, 0.0f}, m = -__builtin_inff(), l = 0.0f;
-  for (int t0 = 0; t0 < geo.len; t0 += 64) {
-    const int t = t0 + lane;
-    float s = -__builtin_inff();
-    if (t < geo.len) {
-      float acc = 0.0f;
-      if (t >= bs && t < be) {
-        const uint16_t* kp = a.k_new + fresh + (t - bs) * fstride;
-        for (int d = 0; d < D; ++d) acc = fmaf(bf_lo(qp[d]), bf_lo(kp[d]), acc);
-      } else {
-        for (int d = 0; d < D; d += 4) {
-          float y[4];
-          decode4<FMT>(*reinterpret_cast<const uint32_t*>(a.k8 + cell + (int64_t)t * D + d), y);
-          for (int e = 0; e < 4; ++e) acc = fmaf(bf_lo(qp[d + e]), y[e], acc);
-        }
-        acc *= a.k_scale[sc0 + ((t + pad) >> a.lt)];
-      }
-      s = acc * a.scale_log2e;
-    }
-    float mx = s;
-    for (int x = 32; x >= 1; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float mn = fmaxf(m, mx), alpha = exp2f(m - mn);
-    const float p = t < geo.len ? exp2f(s - mn) : 0.0f;
-    float ps = p;
-    for (int x = 32; x >= 1; x >>= 1) ps += __shfl_xor(ps, x, 64);
-    l = l * alpha + ps;
-    o[0] *= alpha;
-    o[1] *= alpha;
-    m = mn;
-    const int nk = min(64, geo.len - t0);
-    for (int x = 0; x < nk; ++x) {
-      const float pt = __shfl(p, x, 64);
-      const int tk = t0 + x;
-      for (int u = 0; u < 2; ++u) {
-        const int d = lane + 64 * u;
-        if (d >= D) continue;
-        float v;
-        if (tk >= bs && tk < be) {
-          v = bf_lo(a.v_new[fresh + (tk - bs) * fstride + d]);
-        } else {
-          float y[4];
-          decode4<FMT>(a.v8[cell + (int64_t)tk * D + d], y);
-          v = y[0] * a.v_scale[sc0 + ((tk + pad) >> a.lt)];
-        }
-        o[u] = fmaf(pt, v, o[u]);
-      }
-    }
+  if (r >= a.G * a.L) return;
+  const int jo = r / a.G;
+  const float inv = r < a.G * B ? 1.0f / lt_ : 0.0f;
+  uint16_t* op = a.out + (((int64_t)it.req * a.L + jo) * a.Hq + c * a.G + (r - jo * a.G)) * D + 4 * g;
+  typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int k = 0; k < D / 8; ++k) {
+    const f32x16_t& x = o[k >> 2];
+    const int e = 4 * (k & 3);
+    *reinterpret_cast<v2u*>(op + 8 * k) = v2u{pack_bf16(x[e] * inv, x[e + 1] * inv), pack_bf16(x[e + 2] * inv, x[e + 3] * inv)};
   }
-  for (int u = 0; u < 2; ++u)
-    if (lane + 64 * u < D) op[lane + 64 * u] = (uint16_t)pack_bf16(o[u] / l, 0.0f);
+}
+
+// Joins the pieces of a split row: one wave per (row, row tile, group of 4
+// features), folding the pieces' partials by their running maxima, eight loads in
+// flight.
+template <int D>
+__global__ __launch_bounds__(256) void k_qattn_merge(QAttnArgs a) {
+  constexpr int NG = D / 8, CH = kMergeBatch;
+  const int wv = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (wv >= a.n_merge * a.RTW * NG) return;
+  const int k = wv % NG, t = wv / NG % a.RTW;
+  const QMerge mg = a.merges[wv / NG / a.RTW];
+  const int64_t stride = (int64_t)a.RTW * part_wave_floats(D);
+  const float* pw = a.parts + ((int64_t)mg.part0 * a.RTW + t) * part_wave_floats(D);
+  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -__builtin_inff(), l = 0.0f;
+  for (int p0 = 0; p0 < mg.nparts; p0 += CH) {
+    float mp[CH], lp[CH];
+    f32x4_t op[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const bool ok = p0 + i < mg.nparts;
+      const float* pp = pw + (ok ? p0 + i : p0) * stride;
+      mp[i] = ok ? pp[NG * 256 + lane] : -__builtin_inff();
+      lp[i] = pp[NG * 256 + 64 + lane];
+      op[i] = *reinterpret_cast<const f32x4_t*>(pp + (k * 64 + lane) * 4);
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) mn = fmaxf(mn, mp[i]);
+    const float sa = __builtin_amdgcn_exp2f(m - mn);
+    l *= sa;
+    acc *= sa;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const float sb = __builtin_amdgcn_exp2f(mp[i] - mn);     // 0 for the padding entries
+      l = fmaf(lp[i], sb, l);
+      acc += op[i] * sb;
+    }
+    m = mn;
+  }
+  const int r = (mg.rt0 + t) * 32 + (lane & 31);
+  if (r >= a.G * a.L) return;
+  const int j = r / a.G;
+  const float inv = r < a.G * mg.B ? 1.0f / l : 0.0f;
+  uint16_t* op = a.out + (((int64_t)mg.req * a.L + j) * a.Hq + mg.kvh * a.G + (r - j * a.G)) * D + 8 * k + 4 * (lane >> 5);
+  typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+  *reinterpret_cast<v2u*>(op) = v2u{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+}
+
+template <int FMT, int D>
+void attend(const QAttnArgs& a, hipStream_t s) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_items), dim3((unsigned)(64 * a.RTW)), 0, s, a);
+  };
+  const bool uni = a.lt >= 5;
+  if (a.RTW == 1)
+    uni ? go(k_qattn<FMT, D, 1, true>) : go(k_qattn<FMT, D, 1, false>);
+  else if (a.RTW <= 4)
+    uni ? go(k_qattn<FMT, D, 4, true>) : go(k_qattn<FMT, D, 4, false>);
+  else
+    uni ? go(k_qattn<FMT, D, 8, true>) : go(k_qattn<FMT, D, 8, false>);
+  if (a.n_merge)
+    hipLaunchKernelGGL(k_qattn_merge<D>, dim3((unsigned)((a.n_merge * a.RTW * (D / 8) + 3) / 4)), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_qattn(const QAttnArgs& a, bs_qformat fmt, hipStream_t s) {
-  const int jblocks = (a.L + 3) / 4;
-  const dim3 grid((unsigned)((int64_t)a.n * a.Hq * jblocks));
-  if (fmt == BS_E4M3)
-    hipLaunchKernelGGL(k_qattn<BS_E4M3>, grid, dim3(256), 0, s, a, jblocks);
+  if (a.D == 64)
+    fmt == BS_E4M3 ? attend<BS_E4M3, 64>(a, s) : attend<BS_I8, 64>(a, s);
   else
-    hipLaunchKernelGGL(k_qattn<BS_I8>, grid, dim3(256), 0, s, a, jblocks);
+    fmt == BS_E4M3 ? attend<BS_E4M3, 128>(a, s) : attend<BS_I8, 128>(a, s);
   return hipGetLastError();
 }
 
