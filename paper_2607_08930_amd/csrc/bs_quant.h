@@ -36,14 +36,10 @@ struct NormRopeArgs {
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, bs_dtype dt, int n, int max_tokens, hipStream_t s);
 
-// Quantising: token t of head h of request i is read at
-//   box   (block == 0)  src[row_i][h][off_i + t]     t in [0, len_i)
-//   block (block == 1)  src[i][t - s_i][h]           t in [s_i, s_i + B_i)
-// and written to the cache cell of the box either way.
+// Whole rows of the box: k, v [R][Hkv][W][D] of the call's type
 struct QuantArgs {
   const bs_req_desc* reqs;
-  int L, Hkv, W, S, lt;
-  int block;
+  int Hkv, W, S, lt;
   const void* k;
   const void* v;
   uint8_t* k8;               // [R][Hkv][W][D]
@@ -51,7 +47,7 @@ struct QuantArgs {
   float* k_scale;            // [R][Hkv][S]
   float* v_scale;
 };
-hipError_t launch_kv_quantize(const QuantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_tokens,
+hipError_t launch_kv_quantize(const QuantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_len,
                               hipStream_t s);
 
 struct DequantArgs {
@@ -92,18 +88,20 @@ constexpr int kQRowTiles = 8;   // most 32-row tiles (waves) per workgroup
 
 struct QAttnArgs {
   const QItem* items;
+  const QItem* rows;         // [n]: the requests, whole
   const QMerge* merges;
-  int n_items, n_merge;
+  int n, n_items, n_merge;
   int RTW;                   // row tiles per workgroup
   int L, Hq, Hkv, D, G, W, S, lt;
   float scale_log2e;
   const uint16_t* q;         // [n][L][Hq][D] bf16
   const uint16_t* k_new;     // [n][L][Hkv][D]
   const uint16_t* v_new;
-  const uint8_t* k8;
-  const uint8_t* v8;
-  const float* k_scale;
-  const float* v_scale;
+  uint8_t* k8;               // written at the block's cells and groups only, with write_back
+  uint8_t* v8;
+  float* k_scale;
+  float* v_scale;
+  int write_back;
   uint16_t* out;             // [n][L][Hq][D]
   float* parts;              // part_wave_floats(D) per wave of a partial slot
 };
@@ -146,6 +144,78 @@ __host__ __device__ constexpr float quant_max() { return FMT == BS_E4M3 ? kE4m3M
 
 __device__ inline float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+template <int V>
+struct QInt {
+  static constexpr int value = V;
+};
+
+// The larger of x and its value in the lane that differs in bit O (compile time),
+// where the lanes below that bit agree already: swaps within the VALU, no LDS round
+// trip (a mirror reaches a lane that holds the same as the one with the bit flipped).
+template <int O>
+__device__ inline float max_across(float x) {
+  const int v = (int)__float_as_uint(x);
+  if constexpr (O == 1)
+    return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true)));     // quad 1 0 3 2
+  else if constexpr (O == 2)
+    return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true)));     // quad 2 3 0 1
+  else if constexpr (O == 4)
+    return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true)));    // mirror of 8
+  else if constexpr (O == 8)
+    return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, true)));    // mirror of 16
+  else if constexpr (O == 16) {
+    const auto p = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  } else {
+    const auto p = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+}
+
+// Group maxima of a wave's rows: lane group i (GS lanes a row) of step p holds row
+// p * RS + i, RS = 64 / GS, groups of T = 1 << lt rows from row 0 on; top[p] is the
+// lane's own maximum on entry and its row's group's on return.
+template <int GS, int RP>
+__device__ inline void group_tops(float (&top)[RP], int lt) {
+  constexpr int RS = 64 / GS;
+  const int T = 1 << lt;
+  auto stage = [&](auto o) {
+    if (GS * T > decltype(o)::value) {          // uniform
+#pragma unroll
+      for (int i = 0; i < RP; ++i) top[i] = max_across<decltype(o)::value>(top[i]);
+    }
+  };
+  stage(QInt<1>{});
+  stage(QInt<2>{});
+  stage(QInt<4>{});
+  stage(QInt<8>{});
+  stage(QInt<16>{});
+  stage(QInt<32>{});
+  // groups of several steps
+#pragma unroll
+  for (int b = 1; b < RP; b <<= 1)
+    if (T > b * RS) {
+#pragma unroll
+      for (int i = 0; i < RP; ++i)
+        if (!(i & b)) top[i] = top[i | b] = fmaxf(top[i], top[i | b]);
+    }
+}
+
+// 16 numbers, x(e), as codes in units of m / Q
+template <int FMT, class X>
+__device__ inline v4u encode16(float m, X x) {
+  // x * (Q / m) is rounded by itself, not within the addition that rounds it to an integer
+#pragma clang fp contract(off)
+  const float inv = quant_max<FMT>() / m;
+  v4u w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float y[4] = {x(4 * k) * inv, x(4 * k + 1) * inv, x(4 * k + 2) * inv, x(4 * k + 3) * inv};
+    w[k] = encode4<FMT>(y);
+  }
+  return w;
+}
+
 typedef __bf16 qb2 __attribute__((ext_vector_type(2)));
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(qf2{lo, hi}, qb2));

@@ -940,15 +940,16 @@ size_t qattn_part_bytes(int parts, const QRows& q, int D) {
   return (size_t)parts * q.per * part_wave_floats(D) * sizeof(float);
 }
 
-// meta = {items, item count, merges, merge count, partial slots, descriptors}
+// meta = {items, item count, merges, merge count, partial slots, whole rows}
 void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, bool split) {
   const QRows q = qattn_rows(L, Hq, Hkv);
   const int cap = split ? qattn_cap(reqs, n, L, Hkv, q) : 0;
   std::vector<QItem> items;
+  std::vector<QItem> rows((size_t)n);
   std::vector<QMerge> merges;
   int parts = 0;
   for (int i = 0; i < n; ++i) {
-    const QItem row = qattn_row(reqs[i], i, L);
+    const QItem row = rows[i] = qattn_row(reqs[i], i, L);
     const int nt = qattn_tiles(row), np = cap > 0 && nt > cap ? (nt + cap - 1) / cap : 1;
     for (int h = 0; h < Hkv; ++h)
       for (int gr = 0; gr < q.groups; ++gr) {
@@ -973,7 +974,7 @@ void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int H
   blob.meta[2] = (int)blob.add(merges.data(), sizeof(QMerge) * merges.size());
   blob.meta[3] = (int)merges.size();
   blob.meta[4] = parts;
-  blob.meta[5] = (int)blob.add(reqs, sizeof(bs_req_desc) * n);
+  blob.meta[5] = (int)blob.add(rows.data(), sizeof(QItem) * rows.size());
 }
 
 int longest_row(const bs_req_desc* reqs, int n) {
@@ -1456,7 +1457,7 @@ int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int 
   if (st) return st;
   QuantArgs a{};
   a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
-  a.L = L; a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
+  a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.k = k; a.v = v;
   a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
   a.k_scale = k_scale; a.v_scale = v_scale;
@@ -1544,26 +1545,19 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   a.n_items = meta[1];
   a.merges = reinterpret_cast<const QMerge*>(base + meta[2]);
   a.n_merge = meta[3];
+  a.rows = reinterpret_cast<const QItem*>(base + meta[5]);
+  a.n = n;
   a.parts = static_cast<float*>(ws);
   a.RTW = q_rows.per;
   a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.scale_log2e = (scale > 0.0f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   a.q = static_cast<const uint16_t*>(q);
   a.k_new = static_cast<const uint16_t*>(k_new); a.v_new = static_cast<const uint16_t*>(v_new);
-  a.k8 = static_cast<const uint8_t*>(k8); a.v8 = static_cast<const uint8_t*>(v8);
+  a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
   a.k_scale = k_scale; a.v_scale = v_scale;
+  a.write_back = write_back ? 1 : 0;
   a.out = static_cast<uint16_t*>(out);
-  hipError_t e = launch_qattn(a, fmt, s);
-  if (e == hipSuccess && write_back) {
-    QuantArgs w{};
-    w.reqs = reinterpret_cast<const bs_req_desc*>(base + meta[5]);
-    w.L = L; w.Hkv = Hkv; w.W = W; w.S = S; w.lt = a.lt; w.block = 1;
-    w.k = k_new; w.v = v_new;
-    w.k8 = static_cast<uint8_t*>(k8); w.v8 = static_cast<uint8_t*>(v8);
-    w.k_scale = k_scale; w.v_scale = v_scale;
-    e = launch_kv_quantize(w, BS_BF16, fmt, D, n, L, s);
-  }
-  return end(c, call, s, e, "8-bit attention launch");
+  return end(c, call, s, launch_qattn(a, fmt, s), "8-bit attention launch");
 }
 
 // ------------------------------------------------------------------ norm and rotation

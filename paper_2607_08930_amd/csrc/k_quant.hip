@@ -37,25 +37,18 @@ struct Sixteen {
 // One wave quantises RS * RP tokens (a multiple of T) of one head of K or V.
 template <typename E, int FMT, int D, int RP>
 __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
-  // x * (Q / a) is rounded by itself, not within the addition that rounds it to an integer
-#pragma clang fp contract(off)
   constexpr int GS = D / 16;        // lanes per token
   constexpr int RS = 64 / GS;       // tokens per step
   constexpr int CT = RS * RP;       // tokens per wave
   const bs_req_desc r = a.reqs[blockIdx.y];
   const int h = blockIdx.z >> 1, tensor = blockIdx.z & 1;
-  const Geo geo = geo_of(r, a.L);
   const int lane = threadIdx.x & 63, T = 1 << a.lt;
-  const int pad = group_pad(r.p, a.lt);
-  const int tlo = a.block ? geo.s : 0, thi = a.block ? geo.s + geo.B : geo.len;
-  // virtual token v = t + pad: group v >> lt; the first chunk starts at a group border
-  const int v0 = ((tlo + pad) & ~(T - 1)) + (blockIdx.x * 4 + (threadIdx.x >> 6)) * CT;
-  if (v0 >= thi + pad) return;
-  const int64_t cell0 = (((int64_t)r.row * a.Hkv + h) * a.W + r.off) * D;
-  const E* src = static_cast<const E*>(tensor ? a.v : a.k);
-  const int64_t sstride = a.block ? (int64_t)a.Hkv * D : D;
-  src += a.block ? ((int64_t)blockIdx.y * a.L * a.Hkv + h) * D - geo.s * sstride : cell0;
-  const int col = (lane % GS) * 16;
+  const int pad = group_pad(r.p, a.lt), len = r.p + r.g;
+  // virtual token v = t + pad: group v >> lt
+  const int v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CT;
+  if (v0 >= len + pad) return;
+  const int64_t cell0 = (((int64_t)r.row * a.Hkv + h) * a.W + r.off) * D + (lane % GS) * 16;
+  const E* src = static_cast<const E*>(tensor ? a.v : a.k) + cell0;
 
   Sixteen<E> x[RP];
   float top[RP];
@@ -63,8 +56,8 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
     const int t = v0 + i * RS + lane / GS - pad;
-    ok[i] = t >= tlo && t < thi;
-    if (ok[i]) x[i].load(src + t * sstride + col);
+    ok[i] = t >= 0 && t < len;
+    if (ok[i]) x[i].load(src + (int64_t)t * D);
   }
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
@@ -73,33 +66,16 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) top[i] = fmaxf(top[i], fabsf(x[i].get(e)));
     }
-    // over the token's lanes, then over the tokens of the group within this step
-    for (int o = 1; o < GS * min(T, RS); o <<= 1) top[i] = fmaxf(top[i], __shfl_xor(top[i], o, 64));
   }
-  // groups of several steps
-#pragma unroll
-  for (int b = 1; b < RP; b <<= 1)
-    if (T > b * RS) {
-#pragma unroll
-      for (int i = 0; i < RP; ++i)
-        if (!(i & b)) top[i] = top[i | b] = fmaxf(top[i], top[i | b]);
-    }
-  uint8_t* codes = (tensor ? a.v8 : a.k8) + cell0 + col;
+  group_tops<GS>(top, a.lt);
+  uint8_t* codes = (tensor ? a.v8 : a.k8) + cell0;
   float* scales = (tensor ? a.v_scale : a.k_scale) + ((int64_t)r.row * a.Hkv + h) * a.S;
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
     const int v = v0 + i * RS + lane / GS;
     const float m = fmaxf(top[i], kQuantFloor);
-    if (lane % GS == 0 && (v & (T - 1)) == 0 && v < thi + pad) scales[v >> a.lt] = m / quant_max<FMT>();
-    if (!ok[i]) continue;
-    const float inv = quant_max<FMT>() / m;
-    v4u w;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float y[4] = {x[i].get(4 * k) * inv, x[i].get(4 * k + 1) * inv, x[i].get(4 * k + 2) * inv, x[i].get(4 * k + 3) * inv};
-      w[k] = encode4<FMT>(y);
-    }
-    st16(codes + (int64_t)(v - pad) * D, w);
+    if (lane % GS == 0 && (v & (T - 1)) == 0 && v < len + pad) scales[v >> a.lt] = m / quant_max<FMT>();
+    if (ok[i]) st16(codes + (int64_t)(v - pad) * D, encode16<FMT>(m, [&](int e) { return x[i].get(e); }));
   }
 }
 
@@ -141,12 +117,12 @@ __global__ __launch_bounds__(256) void k_kv_dequantize(DequantArgs a) {
 }
 
 template <typename E, int FMT, int D>
-void quantize(const QuantArgs& a, int n, int max_tokens, hipStream_t s) {
+void quantize(const QuantArgs& a, int n, int max_len, hipStream_t s) {
   constexpr int RS = 64 / (D / 16);
   const int T = 1 << a.lt;
   auto go = [&](auto kernel, int rp) {
     const int per = 4 * RS * rp;    // tokens per workgroup
-    const dim3 grid((unsigned)((max_tokens + T - 1 + per - 1) / per), (unsigned)n, (unsigned)(2 * a.Hkv));
+    const dim3 grid((unsigned)((max_len + T - 1 + per - 1) / per), (unsigned)n, (unsigned)(2 * a.Hkv));
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   };
   if (T > 4 * RS)
@@ -162,23 +138,19 @@ void dequantize(const DequantArgs& a, int n, int max_len, hipStream_t s) {
 }
 
 // f(E{}, format, D) with the three as compile-time values
-template <int V>
-struct Int {
-  static constexpr int value = V;
-};
 template <class F>
 void dispatch(bs_dtype dt, bs_qformat fmt, int D, F f) {
-  auto by_d = [&](auto e, auto m) { D == 64 ? f(e, m, Int<64>{}) : f(e, m, Int<128>{}); };
-  auto by_f = [&](auto e) { fmt == BS_E4M3 ? by_d(e, Int<BS_E4M3>{}) : by_d(e, Int<BS_I8>{}); };
+  auto by_d = [&](auto e, auto m) { D == 64 ? f(e, m, QInt<64>{}) : f(e, m, QInt<128>{}); };
+  auto by_f = [&](auto e) { fmt == BS_E4M3 ? by_d(e, QInt<BS_E4M3>{}) : by_d(e, QInt<BS_I8>{}); };
   dt == BS_BF16 ? by_f(uint16_t{}) : by_f(float{});
 }
 
 }  // namespace
 
-hipError_t launch_kv_quantize(const QuantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_tokens,
+hipError_t launch_kv_quantize(const QuantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_len,
                               hipStream_t s) {
   dispatch(dt, fmt, D, [&](auto e, auto m, auto d) {
-    quantize<decltype(e), decltype(m)::value, decltype(d)::value>(a, n, max_tokens, s);
+    quantize<decltype(e), decltype(m)::value, decltype(d)::value>(a, n, max_len, s);
   });
   return hipGetLastError();
 }

@@ -90,6 +90,52 @@ __device__ inline int swz16(int row) {
   return ((row & 3) << 1) | ((row >> 2) & 1);
 }
 
+// The write of the active blocks into the cache: wave u of the launch's last
+// workgroups quantises one tensor of one (request, KV head), with k_kv_quantize's
+// arithmetic. It reads k_new / v_new again instead of the attention's staged copy:
+// inside the attention's waves the same work stood before their first tiles and cost
+// 3 to 5 us a launch, while these waves run where attention waves are done early.
+template <int FMT, int D, int RP>
+__device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
+  constexpr int GS = D / 16, RS = 64 / GS;
+  if (u >= a.n * a.Hkv * 2) return;
+  const int tensor = u & 1, c = (u >> 1) % a.Hkv, i = (u >> 1) / a.Hkv;
+  const QItem it = a.rows[i];
+  const int col = (lane % GS) * 16, T = 1 << a.lt;
+  const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)i * a.L * a.Hkv + c) * D + col;
+  v4u x[RP][2];
+  float top[RP];
+#pragma unroll
+  for (int p = 0; p < RP; ++p) {
+    // rows past B repeat the last one: it counts for no group that is stored
+    const uint16_t* xp = src + (int64_t)min(p * RS + lane / GS, it.B - 1) * a.Hkv * D;
+    x[p][0] = ld16(xp);
+    x[p][1] = ld16(xp + 8);
+  }
+#pragma unroll
+  for (int p = 0; p < RP; ++p) {
+    top[p] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top[p] = fmaxf(top[p], fmaxf(fabsf(bf_lo(x[p][e >> 2][e & 3])), fabsf(bf_hi(x[p][e >> 2][e & 3]))));
+  }
+  group_tops<GS>(top, a.lt);
+  const int64_t row_head = (int64_t)it.row * a.Hkv + c;
+  const int tpad = it.pad & (T - 1);
+  uint8_t* codes = (tensor ? a.v8 : a.k8) + (row_head * a.W + it.off + it.s) * D + col;
+  float* scales = (tensor ? a.v_scale : a.k_scale) + row_head * a.S + ((it.s + tpad) >> a.lt);
+#pragma unroll
+  for (int p = 0; p < RP; ++p) {
+    const int row = p * RS + lane / GS;
+    if (row >= it.B) continue;
+    const float m = fmaxf(top[p], kQuantFloor);
+    if (col == 0 && (row & (T - 1)) == 0) scales[row >> a.lt] = m / quant_max<FMT>();
+    st16(codes + (int64_t)row * D, encode16<FMT>(m, [&](int e) {
+           const uint32_t y = x[p][e >> 3][(e >> 1) & 3];
+           return e & 1 ? bf_hi(y) : bf_lo(y);
+         }));
+  }
+}
+
 // Tiles and ring of a workgroup of up to MAXW waves
 template <int MAXW>
 struct Shape {
@@ -111,8 +157,16 @@ __global__ __launch_bounds__(64 * MAXW, MAXW == 1 ? 1 : 2) void k_qattn(QAttnArg
   static_assert(KT / RPB % NI == 0, "issuing waves split a tile evenly");
   __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB];
 
-  const QItem it = a.items[blockIdx.x];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int)blockIdx.x >= a.n_items) {
+    const int u = ((int)blockIdx.x - a.n_items) * a.RTW + w;
+    if (MAXW > 1 && a.L > 32)
+      quantize_block<FMT, D, D / 16>(a, u, threadIdx.x & 63);
+    else
+      quantize_block<FMT, D, D / 32>(a, u, threadIdx.x & 63);
+    return;
+  }
+  const QItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31, q16 = lane >> 4, j16 = lane & 15;
   const int c = it.kvh, B = it.B, pad = it.pad, seam = it.s + it.pad, lt = a.lt;
   const int v0 = it.v0 ? it.v0 : pad & ~(KT - 1), v1 = it.v1;   // virtual keys of this piece
@@ -428,7 +482,8 @@ __global__ __launch_bounds__(256) void k_qattn_merge(QAttnArgs a) {
 template <int FMT, int D>
 void attend(const QAttnArgs& a, hipStream_t s) {
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_items), dim3((unsigned)(64 * a.RTW)), 0, s, a);
+    const int wb = a.write_back ? (a.n * a.Hkv * 2 + a.RTW - 1) / a.RTW : 0;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.n_items + wb)), dim3((unsigned)(64 * a.RTW)), 0, s, a);
   };
   const bool uni = a.lt >= 5;
   if (a.RTW == 1)
