@@ -163,9 +163,16 @@ def _host(arr, dtype):
     return a
 
 
+# The current stream's handle without building a Stream object (2.75 us a call
+# against 0.2), where this torch has the two functions that its own compiler uses.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_cur_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
     if stream is None:
-        import torch
+        if _raw_stream is not None and _cur_device is not None and torch.cuda.is_initialized():
+            return _raw_stream(_cur_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream

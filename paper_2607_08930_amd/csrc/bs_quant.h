@@ -92,6 +92,7 @@ struct QAttnArgs {
   const QMerge* merges;
   int n, n_items, n_merge;
   int RTW;                   // row tiles per workgroup
+  int KS;                    // RTW = 1: waves that share a row's keys (8, 4 or 2)
   int L, Hq, Hkv, D, G, W, S, lt;
   float scale_log2e;
   const uint16_t* q;         // [n][L][Hq][D] bf16

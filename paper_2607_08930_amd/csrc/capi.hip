@@ -51,11 +51,19 @@ struct Slot {
 
 thread_local std::string g_err;
 
-uint64_t fnv1a(const void* p, size_t n) {
+// Hash of a slot's key (keys with equal hashes are compared), eight bytes at a time
+uint64_t key_hash(const void* p, size_t n) {
   const unsigned char* b = static_cast<const unsigned char*>(p);
-  uint64_t h = 1469598103934665603ull;
-  for (size_t i = 0; i < n; ++i) h = (h ^ b[i]) * 1099511628211ull;
-  return h ^ n;
+  uint64_t h = 1469598103934665603ull ^ n;
+  size_t i = 0;
+  for (; i + 8 <= n; i += 8) {
+    uint64_t v;
+    std::memcpy(&v, b + i, 8);
+    h = (h ^ v) * 0x9e3779b97f4a7c15ull;
+    h ^= h >> 29;
+  }
+  for (; i < n; ++i) h = (h ^ b[i]) * 1099511628211ull;
+  return h;
 }
 
 }  // namespace
@@ -168,6 +176,7 @@ struct Blob {
 struct Key {
   std::vector<unsigned char> b;
   Key(char tag, std::initializer_list<int64_t> params, const void* data, size_t n) {
+    b.reserve(1 + 8 * params.size() + n);
     b.push_back(static_cast<unsigned char>(tag));
     for (int64_t v : params) push(&v, sizeof v);
     push(data, n);
@@ -226,7 +235,7 @@ int take_slot(bs_ctx* c, Slot** out) {
 // upload it into a slot no queued work reads (take_slot).
 template <class Make>
 int upload(bs_ctx* c, hipStream_t s, const Key& key, Make make, Slot** out) {
-  const uint64_t hv = fnv1a(key.b.data(), key.b.size());
+  const uint64_t hv = key_hash(key.b.data(), key.b.size());
   ++c->tick;
   for (auto& p : c->slots) {
     Slot& sl = *p;
@@ -311,7 +320,7 @@ int begin(bs_ctx* c, hipStream_t s, const Key& key, Make make, Call* call) {
   if (e != hipSuccess) return hip_fail(c, e, "hipStreamIsCapturing");
   if (cap == hipStreamCaptureStatusNone) return upload(c, s, key, make, &call->slot);
   call->captured = true;
-  const uint64_t hv = fnv1a(key.b.data(), key.b.size());
+  const uint64_t hv = key_hash(key.b.data(), key.b.size());
   for (auto& p : c->slots) {
     Slot& sl = *p;
     if (!sl.live || sl.hash != hv || sl.key != key.b) continue;
@@ -925,25 +934,83 @@ QItem qattn_row(const bs_req_desc& r, int i, int L) {
   return it;
 }
 
-PlanShape qattn_shape(const QRows& q) { return q.per == 1 ? PlanShape{kMhaWaves, 2.0, kMergePerPartWave} : PlanShape{1, 1.3, kMergePerPartShared}; }
-
 int qattn_tiles(const QItem& it) { return std::max(1, (it.nv + kQTile - 1) / kQTile); }
 
-// Longest piece in tiles, or 0 to leave every row whole
-int qattn_cap(const bs_req_desc* reqs, int n, int L, int Hkv, const QRows& q) {
+// How a launch cuts its rows: rows of more than `cap` 64-key tiles into even pieces
+// of at most that (0: none); `ks`: waves that share a row's keys, for heads of one
+// row tile.
+struct QPlan {
+  int cap, ks;
+};
+
+// Waves per workgroup of whole rows: a CU holds eight waves, so few rows take eight
+// each, and a full machine two. Measured with 8 / 4 / 2 (LLaDA-8B heads of 320 to 768
+// keys, e4m3, us): 32 rows 8.5 / 9.2 / 12.8, 256: 14.0 / 15.5 / 21.9; 384: 21.7 / 18.4
+// / 24.1, 512: 25.8 / 20.1 / 25.4; 768: 37.5 / 32.8 / 32.1, 1024: 48.9 / 39.7 / 36.2,
+// 1536: 72.3 / 56.8 / 56.5.
+int qattn_waves(size_t items) { return items <= 256 ? 8 : items <= 512 ? 4 : 2; }
+
+// One row tile: the time of a launch of `items` pieces, the longest of `longest`
+// tiles, `total` in all, in us at D = 128. A tile passes through a workgroup in
+// 0.42 us with eight waves (0.78 with four, 1.45 with two: its ring's bytes over the
+// memory's latency), through the whole machine in 3.15 ns (16 KiB at 5.2 TB/s), and the
+// two bounds meet gradually. Beside them 5 us to start and end, 5 for a merge launch and
+// 4 ns a partial. Against 60 measured launches (1 to 48 LLaDA-8B requests, 1 to 40
+// single-token batches of 2512 to 8512 keys, 1 to 4 rows of 8256 and 16256; whole and
+// in pieces of 2 to 48 tiles) within 15%.
+double qattn_estimate(size_t items, int longest, double total, int parts, int ks) {
+  const double c = ks == 8 ? 0.42 : ks == 4 ? 0.78 : 1.45;
+  const size_t slots = (size_t)kPlanCUs * 8 / ks;
+  // past one round a workgroup's place takes its share of the tiles, then half a piece more
+  const double run = items <= slots ? longest : std::max((double)longest, total / slots + 0.5 * total / items);
+  return 5.0 + std::hypot(c * run, 3.15e-3 * total) + (parts ? 5.0 + 4e-3 * parts : 0.0);
+}
+
+QPlan qattn_plan(const bs_req_desc* reqs, int n, int L, int Hkv, const QRows& q) {
   std::vector<Run> runs((size_t)n);
   for (int i = 0; i < n; ++i) runs[i] = Run{qattn_tiles(qattn_row(reqs[i], i, L)), Hkv * q.groups};
-  return split_cap(runs, qattn_shape(q));
+  if (q.per > 1) return QPlan{split_cap(runs, PlanShape{1, 1.3, kMergePerPartShared}), 0};
+  int longest = 0;
+  double total = 0.0;
+  for (const Run& r : runs) {
+    longest = std::max(longest, r.tiles);
+    total += (double)r.tiles * r.count;
+  }
+  const size_t rows = (size_t)n * Hkv;
+  QPlan best{0, qattn_waves(rows)};
+  double least = qattn_estimate(rows, longest, total, 0, best.ks);
+  for (int ks : {8, 4, 2}) {
+    const size_t slots = (size_t)kPlanCUs * 8 / ks;
+    // from an even share of the tiles upwards; the first cap whose pieces fit one round ends it
+    for (int cap = std::max(2, (int)std::ceil(total / slots)); cap < longest; cap += std::max(1, cap / 8)) {
+      size_t items = 0;
+      int parts = 0, piece = 0;
+      for (const Run& r : runs) {
+        const int np = (r.tiles + cap - 1) / cap;
+        items += (size_t)np * r.count;
+        if (np > 1) parts += np * r.count;
+        piece = std::max(piece, (r.tiles + np - 1) / np);
+      }
+      const double t = qattn_estimate(items, piece, total, parts, ks);
+      if (t < least) {
+        least = t;
+        best = QPlan{cap, ks};
+      }
+      if (items <= slots) break;
+    }
+  }
+  return best;
 }
 
 size_t qattn_part_bytes(int parts, const QRows& q, int D) {
   return (size_t)parts * q.per * part_wave_floats(D) * sizeof(float);
 }
 
-// meta = {items, item count, merges, merge count, partial slots, whole rows}
+// meta = {items, item count, merges, merge count, partial slots, whole rows, QPlan::ks}
 void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, bool split) {
   const QRows q = qattn_rows(L, Hq, Hkv);
-  const int cap = split ? qattn_cap(reqs, n, L, Hkv, q) : 0;
+  const QPlan plan = split ? qattn_plan(reqs, n, L, Hkv, q) : QPlan{0, qattn_waves((size_t)n * Hkv)};
+  const int cap = plan.cap;
   std::vector<QItem> items;
   std::vector<QItem> rows((size_t)n);
   std::vector<QMerge> merges;
@@ -959,8 +1026,8 @@ void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int H
         if (np > 1) merges.push_back(QMerge{i, h, it.rt0, it.B, parts, np, {0, 0}});
         for (int k = 0; k < np; ++k) {
           if (np > 1) {
-            it.v0 = k * cap * kQTile;
-            it.v1 = std::min(row.nv, (k + 1) * cap * kQTile);
+            it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
+            it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
             it.part = parts++;
             it.fresh = k == 0;
           }
@@ -975,6 +1042,7 @@ void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int H
   blob.meta[3] = (int)merges.size();
   blob.meta[4] = parts;
   blob.meta[5] = (int)blob.add(rows.data(), sizeof(QItem) * rows.size());
+  blob.meta[6] = plan.ks;
 }
 
 int longest_row(const bs_req_desc* reqs, int n) {
@@ -1497,7 +1565,7 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
 size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D) {
   if (!reqs || n <= 0 || L < 1 || L > 64 || Hkv < 1 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 8 || (D != 64 && D != 128)) return 0;
   const QRows q = qattn_rows(L, Hq, Hkv);
-  const int cap = qattn_cap(reqs, n, L, Hkv, q);
+  const int cap = qattn_plan(reqs, n, L, Hkv, q).cap;
   int parts = 0;
   if (cap > 0)
     for (int i = 0; i < n; ++i) {
@@ -1549,6 +1617,7 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   a.n = n;
   a.parts = static_cast<float*>(ws);
   a.RTW = q_rows.per;
+  a.KS = meta[6];
   a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.scale_log2e = (scale > 0.0f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   a.q = static_cast<const uint16_t*>(q);

@@ -770,9 +770,9 @@ void attend(const QAttnArgs& a, hipStream_t s) {
       go(k_qattn_group<FMT, D, 8, UNI>, a.RTW);
     else if (a.RTW > 1)
       go(k_qattn_group<FMT, D, 4, UNI>, a.RTW);
-    else if (a.n_items <= 256)
+    else if (a.KS == 8)
       go(k_qattn_keys<FMT, D, 8, UNI>, 8);
-    else if (a.n_items <= 512)
+    else if (a.KS == 4)
       go(k_qattn_keys<FMT, D, 4, UNI>, 4);
     else
       go(k_qattn_keys<FMT, D, 2, UNI>, 2);
