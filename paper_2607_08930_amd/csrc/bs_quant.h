@@ -145,9 +145,11 @@ __host__ __device__ constexpr float quant_max() { return FMT == BS_E4M3 ? kE4m3M
 
 __device__ inline float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// compile-time integer passed to a generic lambda
 template <int V>
 struct QInt {
   static constexpr int value = V;
+  __host__ __device__ constexpr operator int() const { return V; }
 };
 
 // The larger of x and its value in the lane that differs in bit O (compile time),

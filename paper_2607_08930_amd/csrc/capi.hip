@@ -1011,31 +1011,46 @@ void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int H
   const QRows q = qattn_rows(L, Hq, Hkv);
   const QPlan plan = split ? qattn_plan(reqs, n, L, Hkv, q) : QPlan{0, qattn_waves((size_t)n * Hkv)};
   const int cap = plan.cap;
-  std::vector<QItem> items;
-  std::vector<QItem> rows((size_t)n);
+  std::vector<QItem> pieces, rows((size_t)n);
   std::vector<QMerge> merges;
   int parts = 0;
   for (int i = 0; i < n; ++i) {
     const QItem row = rows[i] = qattn_row(reqs[i], i, L);
     const int nt = qattn_tiles(row), np = cap > 0 && nt > cap ? (nt + cap - 1) / cap : 1;
-    for (int h = 0; h < Hkv; ++h)
-      for (int gr = 0; gr < q.groups; ++gr) {
+    for (int h = 0; h < Hkv; ++h) {
+      // the pieces of a row's first workgroup take np partial slots, then those of its second, ...
+      if (np > 1)
+        for (int gr = 0; gr < q.groups; ++gr) merges.push_back(QMerge{i, h, gr * q.per, row.B, parts + gr * np, np, {0, 0}});
+      for (int k = 0; k < np; ++k) {
         QItem it = row;
         it.kvh = h;
-        it.rt0 = gr * q.per;
-        if (np > 1) merges.push_back(QMerge{i, h, it.rt0, it.B, parts, np, {0, 0}});
-        for (int k = 0; k < np; ++k) {
-          if (np > 1) {
-            it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
-            it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
-            it.part = parts++;
-            it.fresh = k == 0;
-          }
-          items.push_back(it);
+        if (np > 1) {
+          it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
+          it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
+          it.part = parts + k;
+          it.fresh = k == 0;
         }
+        pieces.push_back(it);
       }
+      if (np > 1) parts += np * q.groups;
+    }
   }
-  std::stable_sort(items.begin(), items.end(), [](const QItem& x, const QItem& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
+  // longest first; the workgroups of a piece, which read the same keys, stand eight
+  // apart, which is the same XCD and its L2
+  std::stable_sort(pieces.begin(), pieces.end(), [](const QItem& x, const QItem& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
+  std::vector<QItem> items;
+  items.reserve(pieces.size() * q.groups);
+  for (size_t b = 0; b < pieces.size(); b += 8)
+    for (int gr = 0; gr < q.groups; ++gr)
+      for (size_t k = b; k < std::min(b + 8, pieces.size()); ++k) {
+        QItem it = pieces[k];
+        it.rt0 = gr * q.per;
+        if (it.part >= 0) {
+          const int nt = qattn_tiles(rows[it.req]);
+          it.part += gr * ((nt + cap - 1) / cap);
+        }
+        items.push_back(it);
+      }
   blob.meta[0] = (int)blob.add(items.data(), sizeof(QItem) * items.size());
   blob.meta[1] = (int)items.size();
   blob.meta[2] = (int)blob.add(merges.data(), sizeof(QMerge) * merges.size());

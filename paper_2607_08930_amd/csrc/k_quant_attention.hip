@@ -26,6 +26,8 @@
 // so neither costs an instruction per key; the row sum takes (sum p') / vs.
 // The weights are rounded to bf16, whose range holds any scale allowed; fp16 would
 // round eight times finer, but a weight times a small scale leaves its range.
+#include <type_traits>
+
 #include "bs_lds.h"
 #include "bs_quant.h"
 
@@ -38,6 +40,9 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4;
 typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
 
@@ -90,50 +95,64 @@ __device__ inline int swz16(int row) {
   return ((row & 3) << 1) | ((row >> 2) & 1);
 }
 
-// The write of the active blocks into the cache: wave u of the launch's last
-// workgroups quantises one tensor of one (request, KV head), with k_kv_quantize's
-// arithmetic. It reads k_new / v_new again instead of the attention's staged copy:
-// inside the attention's waves the same work stood before their first tiles and cost
-// 3 to 5 us a launch, while these waves run where attention waves are done early.
-template <int FMT, int D, int RP>
-__device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
+// The write of one tensor of an active block into the cache, by one wave, with
+// k_kv_quantize's arithmetic: 16 features a lane, row(p) the 16 bf16 numbers of block
+// row p RS + lane / GS (rows past B repeat the last one: it counts for no group that
+// is stored). In a workgroup of several row tiles it reads the block's staged copy,
+// beside the other waves' first MFMAs. With one row tile it would stand before a
+// wave's first tiles and cost 3 to 5 us a launch: there waves of the launch's last
+// workgroups read k_new / v_new again, where attention waves are done early. (Several
+// row tiles the same way: a CU holds one such workgroup, so these would run after
+// the others, 3 us.)
+template <int FMT, int D, int RP, class Row>
+__device__ inline void store_block(const QAttnArgs& a, const QItem& it, int c, int tensor, int lane, Row row) {
   constexpr int GS = D / 16, RS = 64 / GS;
-  if (u >= a.n * a.Hkv * 2) return;
-  const int tensor = u & 1, c = (u >> 1) % a.Hkv, i = (u >> 1) / a.Hkv;
-  const QItem it = a.rows[i];
   const int col = (lane % GS) * 16, T = 1 << a.lt;
-  const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)i * a.L * a.Hkv + c) * D + col;
-  v4u x[RP][2];
   float top[RP];
-#pragma unroll
-  for (int p = 0; p < RP; ++p) {
-    // rows past B repeat the last one: it counts for no group that is stored
-    const uint16_t* xp = src + (int64_t)min(p * RS + lane / GS, it.B - 1) * a.Hkv * D;
-    x[p][0] = ld16(xp);
-    x[p][1] = ld16(xp + 8);
-  }
 #pragma unroll
   for (int p = 0; p < RP; ++p) {
     top[p] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top[p] = fmaxf(top[p], fmaxf(fabsf(bf_lo(x[p][e >> 2][e & 3])), fabsf(bf_hi(x[p][e >> 2][e & 3]))));
+    for (int hh = 0; hh < 2; ++hh) {
+      const v4u x = row(p, hh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top[p] = fmaxf(top[p], fmaxf(fabsf(bf_lo(x[e])), fabsf(bf_hi(x[e]))));
+    }
   }
   group_tops<GS>(top, a.lt);
   const int64_t row_head = (int64_t)it.row * a.Hkv + c;
-  const int tpad = it.pad & (T - 1);
   uint8_t* codes = (tensor ? a.v8 : a.k8) + (row_head * a.W + it.off + it.s) * D + col;
-  float* scales = (tensor ? a.v_scale : a.k_scale) + row_head * a.S + ((it.s + tpad) >> a.lt);
+  float* scales = (tensor ? a.v_scale : a.k_scale) + row_head * a.S + ((it.s + (it.pad & (T - 1))) >> a.lt);
 #pragma unroll
   for (int p = 0; p < RP; ++p) {
-    const int row = p * RS + lane / GS;
-    if (row >= it.B) continue;
+    const int r = p * RS + lane / GS;
+    if (r >= it.B) continue;
     const float m = fmaxf(top[p], kQuantFloor);
-    if (col == 0 && (row & (T - 1)) == 0) scales[row >> a.lt] = m / quant_max<FMT>();
-    st16(codes + (int64_t)row * D, encode16<FMT>(m, [&](int e) {
-           const uint32_t y = x[p][e >> 3][(e >> 1) & 3];
+    if (col == 0 && (r & (T - 1)) == 0) scales[r >> a.lt] = m / quant_max<FMT>();
+    const v4u x[2] = {row(p, 0), row(p, 1)};
+    st16(codes + (int64_t)r * D, encode16<FMT>(m, [&](int e) {
+           const uint32_t y = x[e >> 3][(e >> 1) & 3];
            return e & 1 ? bf_hi(y) : bf_lo(y);
          }));
   }
+}
+
+// Unit u of the launch's last workgroups: one tensor of one (request, KV head)
+template <int FMT, int D>
+__device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
+  constexpr int GS = D / 16, RS = 64 / GS, RP = 32 / RS;   // a single row tile: L <= 32
+  if (u >= a.n * a.Hkv * 2) return;
+  const int tensor = u & 1, c = (u >> 1) % a.Hkv, i = (u >> 1) / a.Hkv;
+  const QItem it = a.rows[i];
+  const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)i * a.L * a.Hkv + c) * D + (lane % GS) * 16;
+  v4u x[RP][2];
+#pragma unroll
+  for (int p = 0; p < RP; ++p) {
+    const uint16_t* xp = src + (int64_t)min(p * RS + lane / GS, it.B - 1) * a.Hkv * D;
+    x[p][0] = ld16(xp);
+    x[p][1] = ld16(xp + 8);
+  }
+  store_block<FMT, D, RP>(a, it, c, tensor, lane, [&](int p, int hh) { return x[p][hh]; });
 }
 
 // ---------------------------------------------------------------- softmax state of a wave
@@ -204,7 +223,7 @@ __device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdg
 // 32 c + 16 g + 8 h + e at MFMA 2 c + h. Rows past the block's repeat its last one.
 template <int D>
 __device__ inline void load_queries(const QAttnArgs& a, const QItem& it, int r, int g, bf16x8_t (&qb)[D / 16]) {
-  const int rq = min(r, a.G * it.B - 1), j = rq / a.G;
+  const int rq = min(r, a.G * it.B - 1), j = (int)(((float)rq + 0.5f) * (1.0f / (float)a.G));
   const uint16_t* qp = a.q + (((int64_t)it.req * a.L + j) * a.Hq + it.kvh * a.G + (rq - j * a.G)) * D + 16 * g;
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) qb[kk] = __builtin_bit_cast(bf16x8_t, ld16(qp + 32 * (kk >> 1) + 8 * (kk & 1)));
@@ -225,18 +244,33 @@ __device__ inline bf16x8_t fresh_v(const uint8_t* vt, int i, int lane) {
   return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Four output features (group k: 8 k + 4 g ..) of row r, or zeros behind the block
+// Output row r = j G + h' of a (request, KV head). r / G by a product: exact for r < 512.
 template <int D>
-__device__ inline void store_out(const QAttnArgs& a, int req, int kvh, int B, int r, int k, int g, f32x4_t x, float l) {
-  if (r >= a.G * a.L) return;
-  const int j = r / a.G;
-  const float inv = r < a.G * B ? 1.0f / l : 0.0f;
-  uint16_t* op = a.out + (((int64_t)req * a.L + j) * a.Hq + kvh * a.G + (r - j * a.G)) * D + 8 * k + 4 * g;
+__device__ inline uint16_t* out_row(const QAttnArgs& a, int req, int kvh, int r, float rg) {
+  const int j = (int)(((float)r + 0.5f) * rg);
+  return a.out + (((int64_t)req * a.L + j) * a.Hq + kvh * a.G + (r - j * a.G)) * D;
+}
+
+// Stores of a row tile leave as whole rows, 16 bytes a lane, over LDS (8 KiB at D =
+// 128): straight from the accumulators they are 8 bytes a lane, which took 5 us of
+// the 64 Dream-7B requests' 59. Features 8 k + 4 g .. + 3 of column n:
+template <int D>
+__device__ inline void stage_out(uint8_t* tile, int n, int k, int g, f32x4_t x, float inv, bool on) {
   typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-  // a row behind the block is zero whatever its unused column held
-  const bool on = r < a.G * B;
   const uint32_t w0 = pack_bf16(x[0] * inv, x[1] * inv), w1 = pack_bf16(x[2] * inv, x[3] * inv);
-  *reinterpret_cast<v2u*>(op) = on ? v2u{w0, w1} : v2u{0, 0};
+  // a row behind the block is zero whatever its unused column held
+  *reinterpret_cast<v2u*>(tile + n * D * 2 + ((k ^ (n & (D / 8 - 1))) * 16) + 8 * g) = on ? v2u{w0, w1} : v2u{0, 0};
+}
+// 16-byte pieces first, first + step, ... of the tile's rows r0 ..
+template <int D>
+__device__ inline void send_out(const QAttnArgs& a, int req, int kvh, int r0, const uint8_t* tile, int first, int step) {
+  const float rg = 1.0f / (float)a.G;
+#pragma unroll 4
+  for (int x = first; x < 32 * (D / 8); x += step) {
+    const int row = x / (D / 8), ch = x % (D / 8), r = r0 + row;
+    if (r < a.G * a.L)
+      st16(out_row<D>(a, req, kvh, r, rg) + ch * 8, *reinterpret_cast<const v4u*>(tile + row * D * 2 + ((ch ^ (row & (D / 8 - 1))) * 16)));
+  }
 }
 
 // Where a workgroup's cached keys lie
@@ -284,7 +318,7 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.n_items) {
-    quantize_block<FMT, D, D / 32>(a, ((int)blockIdx.x - a.n_items) * KS + w, threadIdx.x & 63);
+    quantize_block<FMT, D>(a, ((int)blockIdx.x - a.n_items) * KS + w, threadIdx.x & 63);
     return;
   }
   const QItem it = a.items[blockIdx.x];
@@ -483,37 +517,118 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
   __syncthreads();
   float m = -__builtin_inff(), l = 0.0f, wgt[KS];
 #pragma unroll
-  for (int x = 0; x < KS; ++x) m = fmaxf(m, reinterpret_cast<const float*>(rings + x * RING + 4 * SLOT)[lane]);
+  for (int y = 0; y < KS; ++y) m = fmaxf(m, reinterpret_cast<const float*>(rings + y * RING + 4 * SLOT)[lane]);
 #pragma unroll
   for (int x = 0; x < KS; ++x) {
     const float* o = reinterpret_cast<const float*>(rings + x * RING + 4 * SLOT);
     wgt[x] = __builtin_amdgcn_exp2f(o[lane] - m);              // 0 for a wave without keys
     l = fmaf(o[64 + lane], wgt[x], l);
   }
-  float* pw = a.parts + (int64_t)it.part * part_wave_floats(D);
+  constexpr int NG = (D / 8 + KS - 1) / KS;
+  f32x4_t x[NG];
 #pragma unroll
-  for (int k = w; k < D / 8; k += KS) {
-    f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < NG; ++i) {
+    const int k = w + i * KS;
+    x[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int y = 0; y < KS; ++y) x += *reinterpret_cast<const f32x4_t*>(rings + y * RING + (k * 64 + lane) * 16) * wgt[y];
-    if (it.part >= 0)
-      *reinterpret_cast<f32x4_t*>(pw + (k * 64 + lane) * 4) = x;
-    else
-      store_out<D>(a, it.req, it.kvh, it.B, r, k, g, x, l);
+    for (int y = 0; y < KS; ++y) x[i] += *reinterpret_cast<const f32x4_t*>(rings + y * RING + (k * 64 + lane) * 16) * wgt[y];
   }
-  if (it.part >= 0 && w == 0) {
-    pw[D / 8 * 256 + lane] = m;
-    pw[D / 8 * 256 + 64 + lane] = l;
+  if (it.part >= 0) {
+    float* pw = a.parts + (int64_t)it.part * part_wave_floats(D);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) *reinterpret_cast<f32x4_t*>(pw + ((w + i * KS) * 64 + lane) * 4) = x[i];
+    if (w == 0) {
+      pw[D / 8 * 256 + lane] = m;
+      pw[D / 8 * 256 + 64 + lane] = l;
+    }
+    return;
   }
+  __syncthreads();                             // the columns are read: their place takes the rows
+  const bool on = r < a.G * it.B;
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int i = 0; i < NG; ++i) stage_out<D>(rings, n, w + i * KS, g, x[i], inv, on);
+  __syncthreads();
+  send_out<D>(a, it.req, it.kvh, it.rt0 * 32, rings, threadIdx.x, 64 * KS);
 }
 
 // ---------------------------------------------------------------- several row tiles: waves share the ring
-// One wave a row tile; up to MAXW waves share the K/V tiles of a 4-stage ring.
+// The queries as numbers of the codes' own kind, so that codes enter the scores' MFMAs
+// as they are: a query is the sum of two of them, which costs two MFMAs of twice the
+// bf16 rate (no more time) and saves the widening of K (32 to 96 VALU instructions a
+// sub-tile).
+//   e4m3: x 2^k = hi + lo, k putting the row's largest element into [128, 256). hi
+//         holds the four leading bits, lo the four that are left of a bf16 number; lo
+//         loses at most 2^-10, which is 2^-17 of the row's largest.
+//   int8: x 16256 / max|x| rounded to an integer (2^-15 of the largest) = 128 hi + lo;
+//         the sums of hi are shifted by 7 before lo's are added. |128 hi + lo| <=
+//         16256, so the sums stay below 128 * 16256 * 128 < 2^29.
+// Lane (g, n) of operand i holds features 32 i + 16 g .. + 15, as a 16-byte read of K
+// finds them; e4m3's MFMAs take operands 2 j and 2 j + 1 together.
+template <int FMT, int D>
+struct SplitQueries {
+  static constexpr int N = D / 32;
+  i32x4_t hi[N], lo[N];
+  float back;              // a score in these units times this is the score
+
+  __device__ void set(const bf16x8_t (&qb)[D / 16]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qb[i][e]));
+    top = max_across<32>(top);             // the other half-wave holds the row's other features
+    float mul;
+    if constexpr (FMT == BS_E4M3) {
+      const int ex = min(max((int)(__float_as_uint(top) >> 23), 1 + 8), 254);
+      mul = __uint_as_float((uint32_t)(254 + 7 - ex) << 23);        // 2^(7 - exponent)
+      back = __uint_as_float((uint32_t)(ex - 7) << 23);
+    } else {
+      top = fmaxf(top, 1.17549435e-38f);
+      mul = 16256.0f / top;
+      back = top * (1.0f / 16256.0f);
+    }
+    if (!(top < __builtin_inff())) back = __uint_as_float(0x7fc00000u);   // an infinite query: no weight is a number
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (float)qb[2 * i + (w >> 1)][4 * (w & 1) + e] * mul;
+        if constexpr (FMT == BS_E4M3) {
+          const uint32_t h = encode4<FMT>(x);
+          float y[4];
+          decode4<FMT>(h, y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = x[e] - y[e];
+          hi[i][w] = (int)h;
+          lo[i][w] = (int)encode4<FMT>(y);
+        } else {
+          uint32_t h = 0, l = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = (int)__builtin_rintf(x[e]), a = (v + 64) >> 7;
+            h |= ((uint32_t)a & 255u) << (8 * e);
+            l |= ((uint32_t)(v - 128 * a) & 255u) << (8 * e);
+          }
+          hi[i][w] = (int)h;
+          lo[i][w] = (int)l;
+        }
+      }
+  }
+};
+
+// One wave a row tile; up to MAXW waves share the K/V tiles of a 4-stage ring. Five to
+// eight waves also share the widening of V (COOP): the issuing waves write each tile's
+// values once more as bf16 (two buffers), instead of every wave for itself. Fewer waves
+// would not win by that, and the two buffers would keep a second workgroup off the CU.
 template <int MAXW>
 struct Shape {
   static constexpr int KT = 64;                   // keys per stage
   static constexpr int NS = 4;                    // stages
   static constexpr int NI = MAXW == 4 ? 2 : 4;    // waves that issue the DMA
+  static constexpr bool COOP = MAXW > 4;
 };
 
 template <int FMT, int D, int MAXW, bool UNI>
@@ -527,48 +642,54 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
   constexpr int PB = 2 * RPI + 1;                  // DMA instructions per stage and issuing wave
   constexpr int SCB = 2 * KT * 4;                  // bytes of a stage's scales
   static_assert(KT / RPB % NI == 0, "issuing waves split a tile evenly");
-  __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB];
+  constexpr bool COOP = SH::COOP;
+  constexpr int WV = COOP ? KT * D * 2 : 0;        // bytes of a widened V tile
+  // stages, their scales, two widened V tiles
+  __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB + 2 * WV];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x >= a.n_items) {
-    const int u = ((int)blockIdx.x - a.n_items) * a.RTW + w;
-    if (a.L > 32)
-      quantize_block<FMT, D, D / 16>(a, u, threadIdx.x & 63);
-    else
-      quantize_block<FMT, D, D / 32>(a, u, threadIdx.x & 63);
-    return;
-  }
   const QItem it = a.items[blockIdx.x];
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31, q16 = lane >> 4, j16 = lane & 15;
   const Keys<D> keys(a, it);
   const int B = it.B, pad = it.pad, nv = it.nv, v0 = it.v0, v1 = it.v1;
   const int ntiles = (v1 - v0 + KT - 1) / KT;
   const bool issuer = w < NI;
+  const int seam_ = keys.seam;
   const int r = (it.rt0 + w) * 32 + n;
 
   bf16x8_t qb[NKK];
   load_queries<D>(a, it, r, g, qb);
 
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
-  auto issue = [&](int u) {
+  // This lane's 16 bytes of a DMA block: the blocks of a wave lie NI * RPB rows apart, a
+  // multiple of the swizzle's period, so one offset serves them all.
+  static_assert(NI * RPB % 16 == 0, "the swizzle repeats every 16 rows");
+  const int row0 = w * RPB + lane / NC;
+  const uint32_t lane_off = (uint32_t)(row0 * D + (((lane % NC) ^ swz8<D>(row0)) * 16));
+  auto issue = [&](int u, int slot) {
     if (!issuer) return;
-    const int slot = u % NS, vb = v0 + u * KT;
+    const int vb = v0 + u * KT;
     const uint32_t sbase = ring_lds + (uint32_t)(slot * STAGE + w * 1024);
-    const bool whole = keys.whole(vb, KT);
+    const uint32_t ssc = ring_lds + (uint32_t)(NS * STAGE + slot * SCB + (w & 1) * KT * 4);
+    const float* sp = w & 1 ? keys.vs : keys.ks;   // scales by key: K's, then V's; of four waves two fetch the same
+    if (keys.whole(vb, KT)) {
+      const int64_t at = (int64_t)keys.cell(vb) * D;
 #pragma unroll
-    for (int k = 0; k < 2 * RPI; ++k) {
-      const int tensor = k / RPI, blk = k % RPI * NI;
-      const int row = (blk + w) * RPB + lane / NC, chunk = (lane % NC) ^ swz8<D>(row);
-      const uint32_t dst = sbase + (uint32_t)(tensor * TILE + blk * 1024);
-      const uint8_t* cb = tensor ? keys.v : keys.k;
-      if (whole)
-        dma16_sv_once(dst, uniform64(cb + (int64_t)keys.cell(vb) * D), (uint32_t)(row * D + chunk * 16));
-      else
-        dma16_once(dst, cb + (int64_t)keys.cell(keys.clamp(vb + row)) * D + chunk * 16);
+      for (int k = 0; k < 2 * RPI; ++k) {
+        const int tensor = k / RPI, blk = k % RPI * NI;
+        dma16_sv_once(sbase + (uint32_t)(tensor * TILE + blk * 1024), uniform64((tensor ? keys.v : keys.k) + at + blk * 1024), lane_off);
+      }
+      dma4(ssc, sp + (vb >= seam_ ? keys.glen : 0) + ((vb + lane) >> keys.lt));
+    } else {
+      // rows before the first key and past the last repeat one of them (masked later)
+#pragma unroll
+      for (int k = 0; k < 2 * RPI; ++k) {
+        const int tensor = k / RPI, blk = k % RPI * NI, row = blk * RPB + row0;
+        dma16_once(sbase + (uint32_t)(tensor * TILE + blk * 1024),
+                   (tensor ? keys.v : keys.k) + (int64_t)keys.cell(keys.clamp(vb + row)) * D + (int)lane_off % D);
+      }
+      dma4(ssc, sp + keys.group(keys.clamp(vb + lane)));
     }
-    // scales by key: K's, then V's; of four issuing waves two fetch the same
-    dma4(ring_lds + (uint32_t)(NS * STAGE + slot * SCB + (w & 1) * KT * 4),
-         (w & 1 ? keys.vs : keys.ks) + keys.group(keys.clamp(vb + lane)));
   };
   auto wait_stages = [&](int x) {
     if (!issuer) return;
@@ -604,7 +725,7 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
                               (((int64_t)it.req * a.L + min(row, B - 1)) * a.Hkv + it.kvh) * D + chunk * 8;
         dma16(ring_lds + (uint32_t)(foff + b * 1024), src);
       }
-    for (const int lim = min(NS - (2 * FT + STAGE - 1) / STAGE, min(NS - 1, ntiles)); issued < lim; ++issued) issue(issued);
+    for (const int lim = min(NS - (2 * FT + STAGE - 1) / STAGE, min(NS - 1, ntiles)); issued < lim; ++issued) issue(issued, issued);
     wait_stages(issued);
     barrier();
     for (int sub = 0; sub * 32 < B; ++sub) {
@@ -630,9 +751,23 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
         col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fresh_v<D>(kt + FT, i, lane), col.pp[i / NDT],
                                                                  col.o[i % NDT], 0, 0, 0);
     }
+    // K and V by the last two waves: where there are enough, those that issue no DMA, so
+    // that no stage waits for the stores
+    const int wt = w - (a.RTW - 2);
+    if (a.write_back && it.rt0 == 0 && (wt == 0 || wt == 1)) {
+      constexpr int GS = D / 16, RS = 64 / GS;
+      auto row = [&](int p, int hh) {
+        const int x = p * RS + lane / GS, ch = 2 * (lane % GS) + hh;
+        return *reinterpret_cast<const v4u*>(ring + foff + wt * FT + x * D * 2 + ((ch ^ swz16<D>(x)) * 16));
+      };
+      if (RB == 2)
+        store_block<FMT, D, 64 / RS>(a, it, it.kvh, wt, lane, row);
+      else
+        store_block<FMT, D, 32 / RS>(a, it, it.kvh, wt, lane, row);
+    }
     barrier();
   }
-  for (const int lim = min(NS - 1, ntiles); issued < lim; ++issued) issue(issued);
+  for (const int lim = min(NS - 1, ntiles); issued < lim; ++issued) issue(issued, issued);
 
   // LDS byte offsets of this lane's K and V reads (V rows 16 apart and K rows 32
   // apart have the same swizzle)
@@ -643,77 +778,325 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt)
     voff[dt] = TILE + vrow * D + (((2 * dt + (q16 & 1)) ^ swz8<D>(vrow)) * 16) + 8 * (j16 & 1);
+  // the same of a widened V tile (rows 16 apart alike)
+  int woff[NDT][2];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      const int row = 8 * h2 + 4 * (q16 >> 1) + (j16 >> 2), x = 32 * dt + 16 * (q16 & 1) + 4 * (j16 & 3);
+      woff[dt][h2] = NS * STAGE + NS * SCB + row * D * 2 + (((x >> 3) ^ swz16<D>(row)) * 16) + (x & 7) * 2;
+    }
+  // K codes of operand i; the V operand of MFMA i (widened in place without COOP)
+  auto kraw = [&](int slot, int half, int i) {
+    return *reinterpret_cast<const i32x4_t*>(ring + koff[i] + slot * STAGE + half * 32 * D);
+  };
+  auto vraw = [&](int slot, int half, int i) {
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(ring + voff[i % NDT] + slot * STAGE + (2 * half + i / NDT) * 16 * D));
+  };
+  auto vwide = [&](int slot, int half, int i) {
+    const uint8_t* p = ring + (slot & 1) * WV + (2 * half + i / NDT) * 32 * D;
+    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + woff[i % NDT][0]));
+    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + woff[i % NDT][1]));
+    return (bf16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // COOP: issuing wave w widens its share of the tile in `slot`, UN units (row, 16
+  // features) a lane, NI * RPB rows apart: the codes lie where its DMA put them
+  constexpr int UN = COOP ? KT / RPB / NI : 0;
+  const int ch0 = 2 * (lane % NC), wide0 = NS * STAGE + NS * SCB + row0 * D * 2 + ((ch0 ^ swz16<D>(row0)) * 16);
+  auto widen_tile = [&](int slot) {
+#pragma unroll
+    for (int x = 0; x < UN; ++x) {
+      const v4u y = *reinterpret_cast<const v4u*>(ring + lane_off + (slot * STAGE + TILE + x * NI * 1024));
+      uint8_t* to = ring + ((slot & 1) * WV + x * NI * 2048);
+      *reinterpret_cast<bf16x8_t*>(to + wide0) = widen8<FMT>(y[0], y[1]);
+      *reinterpret_cast<bf16x8_t*>(to + (wide0 ^ 16)) = widen8<FMT>(y[2], y[3]);
+    }
+  };
+  auto scales = [&](int slot, int half) { return reinterpret_cast<const float*>(ring + NS * STAGE + slot * SCB) + half * 32; };
+  // x is computed here: keeps the compiler from sinking it past a fence
+  auto pin = [](float& x) { asm volatile("" : "+v"(x)); };
+  // t + the q-th pair of weights, as the MFMA takes them
+  auto add_pair = [&](int q, float t) {
+    const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{col.pp[q >> 2][2 * (q & 3)], col.pp[q >> 2][2 * (q & 3) + 1]}, one, t, false);
+  };
 
-  for (int u = 0; u < ntiles; ++u) {
-    wait_stages(min(NS - 2, ntiles - 1 - u));
-    barrier();
-    if (u + NS - 1 < ntiles) issue(u + NS - 1);
-    const int slot = u % NS;
+  SplitQueries<FMT, D> sq;
+  sq.set(qb);
+  const float qscale = a.scale_log2e * sq.back;
+  // MFMAs of P V; of the scores (e4m3: 64 features each, twice as long)
+  constexpr int NPV = 2 * NDT, NSC = FMT == BS_E4M3 ? D / 32 : D / 16, NSL = NPV + NSC;
+  using acc_t = typename std::conditional<FMT == BS_E4M3, f32x16_t, i32x16_t>::type;
+  const int nsub = v1 > v0 ? (v1 - v0 + 31) / 32 : 0;
+  const int u0 = v0 + 32 <= pad ? 1 : 0;             // a first sub-tile without keys
+  acc_t sA, sB;
+  i32x4_t rk[D / 32];                                // K codes of a sub-tile
+  i32x2_t rv[4];                                     // V codes read three MFMAs ahead
+  bf16x8_t fr[4];                                    // V operands: widened one MFMA ahead, or read three ahead
+  float kf = 0.0f, vs = 0.0f;                        // UNI: scales of the sub-tile whose scores are in
+  auto score_mfma = [&](int i, acc_t& s) {
+    if (i == 0) {
 #pragma unroll
-    for (int sub = 0; sub < SPT; ++sub) {
-      const int vb = v0 + u * KT + sub * 32;
-      if (vb + 32 <= pad || vb >= v1) continue;              // wave-uniform
-      const uint8_t* tile = ring + slot * STAGE + sub * 32 * D;
-      const float* sc = reinterpret_cast<const float*>(ring + NS * STAGE + slot * SCB) + sub * 32;
-      f32x16_t s;
+      for (int rr = 0; rr < 16; ++rr) s[rr] = 0;
+    }
+    if constexpr (FMT == BS_E4M3) {
+      const int j = i >> 1;
+      const i32x4_t& q0 = i & 1 ? sq.lo[2 * j] : sq.hi[2 * j];
+      const i32x4_t& q1 = i & 1 ? sq.lo[2 * j + 1] : sq.hi[2 * j + 1];
+      // scale operands of 0: the MFMA without scales
+      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(__builtin_shufflevector(rk[2 * j], rk[2 * j + 1], 0, 1, 2, 3, 4, 5, 6, 7),
+                                                          __builtin_shufflevector(q0, q1, 0, 1, 2, 3, 4, 5, 6, 7), s, 0, 0, 0, 0, 0, 0);
+    } else {
+      constexpr int N = D / 32;
+      if (i == N) {
 #pragma unroll
-      for (int rr = 0; rr < 16; ++rr) s[rr] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const v4u x = *reinterpret_cast<const v4u*>(tile + koff[i]);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[0], x[1]), qb[2 * i], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[2], x[3]), qb[2 * i + 1], s, 0, 0, 0);
+        for (int rr = 0; rr < 16; ++rr) s[rr] <<= 7;
       }
-      if constexpr (!UNI) {
+      s = __builtin_amdgcn_mfma_i32_32x32x32_i8(rk[i % N], i < N ? sq.hi[i] : sq.lo[i - N], s, 0, 0, 0);
+    }
+  };
+
+  // One sub-tile u, half H of ring slot S (compile time in the unrolled loop, where
+  // every LDS address is then an immediate): ss holds its scores, col.pp the weights
+  // of u - 1; writes the scores of u + 1 to sn and the weights of u to col.pp. Slots
+  // of one MFMA each, in an order fixed by scheduling fences: P V of u - 1 (none for
+  // the first sub-tile), then the scores of u + 1 (of stale LDS contents, and
+  // discarded, for the last); beside them the softmax of u in 16 steps, for a wave's
+  // MFMAs overlap its own VALU work only. With COOP the V operands of an odd
+  // sub-tile's P V are written before the barrier that opens it, so its first steps
+  // stand before its first MFMA, while they are read.
+  auto sub_tile = [&](auto S, auto half_tag, auto first_tag, int u, acc_t& ss, acc_t& sn) {
+    constexpr int H = decltype(half_tag)::value;
+    constexpr bool FIRST = decltype(first_tag)::value != 0, LATE = COOP && H == 1 && !FIRST;
+    const int s0 = S, sp = H ? s0 : (s0 + NS - 1) % NS, sx = H ? (s0 + 1) % NS : s0;
+    if constexpr (H == 1) {
+      // the next tile has landed once only later ones are in flight; past the barrier
+      // every wave is done with the tile before this one, whose slot is refilled
+      const int t = u >> 1;
+      wait_stages(min(t == 0 ? 2 : 1, max(ntiles - 2 - t, 0)));
+      barrier();
+      if (t + 3 < ntiles && t > 0) issue(t + 3, (s0 + NS - 1) % NS);
+      if constexpr (LATE) {
 #pragma unroll
-        for (int qd = 0; qd < 4; ++qd) {
-          const f32x4_t k4 = *reinterpret_cast<const f32x4_t*>(sc + 8 * qd + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * qd + e] *= k4[e] * a.scale_log2e;
-        }
+        for (int i = 0; i < 3; ++i) fr[i] = vwide(sp, 1 - H, i);
       }
-      if (vb < pad || vb + 32 > nv) {
+    } else if constexpr (COOP) {
+      if (issuer) widen_tile(s0);
+    }
+    const int vb = v0 + u * 32;
+    f32x4_t k4[4], v4[4];                            // scales by key: V's are read as they are needed
+    if constexpr (!UNI) {
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) k4[qd] = *reinterpret_cast<const f32x4_t*>(scales(s0, H) + 8 * qd + 4 * g);
+    }
+    const float f = UNI ? kf * qscale : qscale;
+    f32x16_t sc;
+    float m3[4], mx = 0.0f, off = 0.0f, ivs = 0.0f, alpha = 1.0f, sum = 0.0f;
+    bool resc = false;
+    // step st of the softmax of u
+    auto step = [&](int st) {
+      if (!UNI && st >= 2 && st <= 8 && st % 2 == 0)
+        v4[st / 2 - 1] = *reinterpret_cast<const f32x4_t*>(scales(s0, H) + KT + 8 * (st / 2 - 1) + 4 * g);
+      if (st == 0) {
 #pragma unroll
         for (int rr = 0; rr < 16; ++rr) {
-          const int v = vb + key_of(rr, g);
-          if (v < pad || v >= nv) s[rr] = -__builtin_inff();
+          sc[rr] = (float)ss[rr];
+          if constexpr (!UNI) sc[rr] *= k4[rr >> 2][rr & 3];
+        }
+        if (vb < pad || vb + 32 > nv) {
+#pragma unroll
+          for (int rr = 0; rr < 16; ++rr) {
+            const int v = vb + key_of(rr, g);
+            if (v < pad || v >= nv) sc[rr] = -__builtin_inff();
+          }
+        }
+      } else if (st == 1) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          m3[q] = vmax(vmax(sc[3 * q], sc[3 * q + 1]), sc[3 * q + 2]);
+          pin(m3[q]);
+        }
+      } else if (st == 2) {
+        m3[0] = vmax(vmax(sc[12], sc[13]), m3[0]);
+        m3[1] = vmax(vmax(sc[14], sc[15]), m3[1]);
+        m3[0] = vmax(vmax(m3[0], m3[1]), m3[2]);
+        mx = vmax(m3[0], m3[3]) * f;                   // log2 units
+        pin(mx);
+      } else if (st == 3) {
+        // lazily raised running max (Column::raise, with O rescaled after P V of u - 1)
+        resc = __builtin_amdgcn_ballot_w64(mx > col.mtop) != 0;
+        if (resc) {
+          const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+          const float mnew = fmaxf(col.mrun, vmax(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+          alpha = __builtin_amdgcn_exp2f(col.mrun - mnew);
+          col.lsum *= alpha;
+          col.mrun = mnew;
+          col.mtop = mnew + 8.0f;
+        }
+        off = UNI ? col.mrun - __builtin_amdgcn_logf(vs) : col.mrun;
+        if (UNI) ivs = __builtin_amdgcn_rcpf(vs);
+        pin(off);
+      } else if (st < 12) {
+#pragma unroll
+        for (int y = 2 * (st - 4); y < 2 * (st - 4) + 2; ++y) {
+          float p = __builtin_amdgcn_exp2f(fmaf(sc[y], f, -off));
+          if constexpr (!UNI) {
+            col.lsum += p;
+            p *= v4[y >> 2][y & 3];
+          }
+          pin(p);
+          sc[y] = p;
         }
       }
-      if constexpr (UNI) {
-        const float f = uniform(sc[0]) * a.scale_log2e, vs = uniform(sc[KT]);
-        col.raise(top16(s) * f);
-        col.lsum = fmaf(col.weights(s, f, col.mrun - __builtin_amdgcn_logf(vs)), __builtin_amdgcn_rcpf(vs), col.lsum);
-      } else {
-        f32x4_t vs[4];
-#pragma unroll
-        for (int qd = 0; qd < 4; ++qd) vs[qd] = *reinterpret_cast<const f32x4_t*>(sc + KT + 8 * qd + 4 * g);
-        col.raise(top16(s));
-        col.weights_by_key(s, vs);
+      if (st >= 8) {
+        // P V has read the old weights by now
+        const int e = 2 * (st - 8);
+        col.pp[e >> 3][e & 7] = (__bf16)sc[e];
+        col.pp[e >> 3][(e & 7) + 1] = (__bf16)sc[e + 1];
+        if (UNI && e >= 2) sum = add_pair(e / 2 - 1, sum);
       }
+    };
+    constexpr int LEAD = LATE ? 4 : 0;               // steps before the first MFMA
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 2 * NDT; ++i) {
-        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(tile + voff[i % NDT] + i / NDT * 16 * D));
-        col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]), col.pp[i / NDT],
-                                                                 col.o[i % NDT], 0, 0, 0);
+    for (int st = 0; st < LEAD; ++st) step(st);
+    if (LEAD) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NSL; ++i) {
+      // operands: V's three MFMAs ahead (past the end: of the next sub-tile's P V), K's
+      // beside the last MFMAs of P V
+      const int jv = i + 3;
+      if constexpr (COOP) {
+        if (jv >= NSL ? H == 1 : jv < NPV && !FIRST)
+          fr[(jv >= NSL ? jv - NSL : jv) & 3] = jv >= NSL ? vwide(s0, H, jv - NSL) : vwide(sp, 1 - H, jv);
+      } else {
+        if (jv >= NSL)
+          rv[(jv - NSL) & 3] = vraw(s0, H, jv - NSL);
+        else if (jv < NPV && !FIRST)
+          rv[jv & 3] = vraw(sp, 1 - H, jv);
+      }
+      if (i < NPV && i >= NPV - D / 32) rk[i - (NPV - D / 32)] = kraw(sx, 1 - H, i - (NPV - D / 32));
+      if (i < NPV) {
+        if constexpr (!FIRST)
+          col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[COOP ? i & 3 : i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
+      } else {
+        score_mfma(i - NPV, sn);
+      }
+      if constexpr (!COOP) {
+        // widen the next MFMA's operand (past the end: the next sub-tile's first)
+        if (i + 1 < NPV ? !FIRST : i + 1 == NSL) {
+          const i32x2_t& x = rv[i + 1 == NSL ? 0 : (i + 1) & 3];
+          fr[i + 1 == NSL ? 0 : (i + 1) & 1] = widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]);
+        }
+      }
+      // the softmax: steps 0 .. 7 beside P V, 8 .. 15 beside the scores
+      const int b0 = i < NPV ? i * 8 / NPV : 8 + (i - NPV) * 8 / NSC, b1 = i < NPV ? (i + 1) * 8 / NPV : 8 + (i + 1 - NPV) * 8 / NSC;
+#pragma unroll
+      for (int st = b0; st < b1; ++st)
+        if (st >= LEAD) step(st);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!FIRST && i == NPV - 1 && resc) {               // after P V of u - 1, before that of u
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int rr = 0; rr < 16; ++rr) col.o[dt][rr] *= alpha;
+      }
+    }
+    if (FIRST && resc) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr) col.o[dt][rr] *= alpha;
+    }
+    if constexpr (UNI) {
+      col.lsum = fmaf(add_pair(7, sum), ivs, col.lsum);
+      kf = scales(sx, 1 - H)[0];                          // stale for the last sub-tile, and unused
+      vs = scales(sx, 1 - H)[KT];
+    }
+  };
+
+  if (nsub > 0) {
+    wait_stages(min(NS - 2, ntiles - 1));
+    barrier();
+    if (3 < ntiles) issue(3, 3);
+    if (COOP && u0 == 1 && issuer) widen_tile(0);
+    // scores of the first sub-tile
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) rk[i] = kraw(0, u0, i);
+#pragma unroll
+    for (int i = 0; i < NSC; ++i) score_mfma(i, sA);
+    if constexpr (UNI) {
+      kf = scales(0, u0)[0];
+      vs = scales(0, u0)[KT];
+    }
+    using C0 = QInt<0>;
+    using C1 = QInt<1>;
+    // tile 0, then four tiles a trip with compile-time slots, then the rest; the
+    // scores of an even sub-tile are in sA, of an odd one in sB
+    if (u0 == 0) {
+      sub_tile(C0{}, C0{}, C1{}, 0, sA, sB);
+      if (nsub > 1) sub_tile(C0{}, C1{}, C0{}, 1, sB, sA);
+    } else {
+      sB = sA;
+      sub_tile(C0{}, C1{}, C1{}, 1, sB, sA);
+    }
+    int u = 2;
+    for (; u + 7 < nsub; u += 8) {
+      sub_tile(QInt<1>{}, C0{}, C0{}, u, sA, sB);
+      sub_tile(QInt<1>{}, C1{}, C0{}, u + 1, sB, sA);
+      sub_tile(QInt<2>{}, C0{}, C0{}, u + 2, sA, sB);
+      sub_tile(QInt<2>{}, C1{}, C0{}, u + 3, sB, sA);
+      sub_tile(QInt<3>{}, C0{}, C0{}, u + 4, sA, sB);
+      sub_tile(QInt<3>{}, C1{}, C0{}, u + 5, sB, sA);
+      sub_tile(QInt<0>{}, C0{}, C0{}, u + 6, sA, sB);
+      sub_tile(QInt<0>{}, C1{}, C0{}, u + 7, sB, sA);
+    }
+    for (; u < nsub; u += 2) {
+      const int slot = (u >> 1) % NS;
+      sub_tile(slot, C0{}, C0{}, u, sA, sB);
+      if (u + 1 < nsub) sub_tile(slot, C1{}, C0{}, u + 1, sB, sA);
+    }
+    // P V of the last sub-tile
+    const int ul = nsub - 1, sl = (ul >> 1) % NS, hl = ul & 1;
+    if constexpr (COOP) {
+      barrier();                                         // its tile may have been widened just now
+#pragma unroll
+      for (int i = 0; i < NPV; ++i)
+        col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vwide(sl, hl, i), col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
+    } else {
+      // its first operand is widened, the next two are read
+#pragma unroll
+      for (int i = 0; i < NPV; ++i) {
+        if (i + 3 < NPV) rv[(i + 3) & 3] = vraw(sl, hl, i + 3);
+        col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
+        if (i + 1 < NPV) fr[(i + 1) & 1] = widen8<FMT>((uint32_t)rv[(i + 1) & 3][0], (uint32_t)rv[(i + 1) & 3][1]);
       }
     }
   }
 
   col.lsum += __shfl_xor(col.lsum, 32, 64);
   // lane (g, n): O^T[feature 8 k + 4 g + e][query n]
-  float* pw = a.parts + ((int64_t)it.part * a.RTW + w) * part_wave_floats(D);
-#pragma unroll
-  for (int k = 0; k < D / 8; ++k) {
-    const f32x4_t x = {col.o[k >> 2][4 * (k & 3)], col.o[k >> 2][4 * (k & 3) + 1], col.o[k >> 2][4 * (k & 3) + 2], col.o[k >> 2][4 * (k & 3) + 3]};
-    if (it.part >= 0)
-      *reinterpret_cast<f32x4_t*>(pw + (k * 64 + lane) * 4) = x;
-    else
-      store_out<D>(a, it.req, it.kvh, B, r, k, g, x, col.lsum);
-  }
+  auto group4 = [&](int k) {
+    return f32x4_t{col.o[k >> 2][4 * (k & 3)], col.o[k >> 2][4 * (k & 3) + 1], col.o[k >> 2][4 * (k & 3) + 2], col.o[k >> 2][4 * (k & 3) + 3]};
+  };
   if (it.part >= 0) {
+    float* pw = a.parts + ((int64_t)it.part * a.RTW + w) * part_wave_floats(D);
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) *reinterpret_cast<f32x4_t*>(pw + (k * 64 + lane) * 4) = group4(k);
     pw[D / 8 * 256 + lane] = col.mrun;
     pw[D / 8 * 256 + 64 + lane] = col.lsum;
+    return;
   }
+  barrier();                                   // the ring is read: each wave's share takes its rows
+  static_assert(MAXW * 32 * D * 2 <= NS * STAGE, "the row tiles fit the ring");
+  uint8_t* tile = ring + w * 32 * D * 2;
+  const bool on = r < a.G * B;
+  const float inv = 1.0f / col.lsum;
+#pragma unroll
+  for (int k = 0; k < D / 8; ++k) stage_out<D>(tile, n, k, g, group4(k), inv, on);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  send_out<D>(a, it.req, it.kvh, (it.rt0 + w) * 32, tile, lane, 64);
 }
 
 // Joins the pieces of a split row: one wave per (row, row tile, group of 4
@@ -755,13 +1138,20 @@ __global__ __launch_bounds__(256) void k_qattn_merge(QAttnArgs a) {
     }
     m = mn;
   }
-  store_out<D>(a, mg.req, mg.kvh, mg.B, (mg.rt0 + t) * 32 + (lane & 31), k, lane >> 5, acc, l);
+  const int r = (mg.rt0 + t) * 32 + (lane & 31);
+  if (r >= a.G * a.L) return;
+  const float inv = 1.0f / l;
+  typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+  const v2u y = {pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+  *reinterpret_cast<v2u*>(out_row<D>(a, mg.req, mg.kvh, r, 1.0f / (float)a.G) + 8 * k + 4 * (lane >> 5)) =
+      r < a.G * mg.B ? y : v2u{0, 0};
 }
 
 template <int FMT, int D>
 void attend(const QAttnArgs& a, hipStream_t s) {
   auto go = [&](auto kernel, int waves) {
-    const int wb = a.write_back ? (a.n * a.Hkv * 2 + waves - 1) / waves : 0;
+    // one row tile: workgroups that write the blocks into the cache stand last
+    const int wb = a.write_back && a.RTW == 1 ? (a.n * a.Hkv * 2 + waves - 1) / waves : 0;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.n_items + wb)), dim3((unsigned)(64 * waves)), 0, s, a);
   };
   auto by_groups = [&](auto uni_tag) {
