@@ -84,7 +84,7 @@ struct QMerge {
 };
 
 constexpr int kQTile = 64;   // virtual keys per planning unit
-constexpr int kQRowTiles = 8;   // most 32-row tiles (waves) per workgroup
+constexpr int kQRowTiles = 4;   // most 32-row tiles (waves) per workgroup
 
 struct QAttnArgs {
   const QItem* items;

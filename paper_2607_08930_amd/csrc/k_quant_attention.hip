@@ -619,22 +619,18 @@ struct SplitQueries {
   }
 };
 
-// One wave a row tile; up to MAXW waves share the K/V tiles of a 4-stage ring. Five to
-// eight waves also share the widening of V (COOP): the issuing waves write each tile's
-// values once more as bf16 (two buffers), instead of every wave for itself. Fewer waves
-// would not win by that, and the two buffers would keep a second workgroup off the CU.
-template <int MAXW>
-struct Shape {
-  static constexpr int KT = 64;                   // keys per stage
-  static constexpr int NS = 4;                    // stages
-  static constexpr int NI = MAXW == 4 ? 2 : 4;    // waves that issue the DMA
-  static constexpr bool COOP = MAXW > 4;
-};
-
-template <int FMT, int D, int MAXW, bool UNI>
-__global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
-  using SH = Shape<MAXW>;
-  constexpr int KT = SH::KT, NS = SH::NS, NI = SH::NI, SPT = KT / 32;
+// One wave a row tile; up to four waves share the K/V tiles of a 4-stage ring, and two
+// such workgroups a CU (two waves per SIMD). Eight waves in one workgroup a CU, which
+// read each tile once and shared the widening of V, took 67 us instead of 77 for 64
+// Dream-7B rows of equal length, but 57 instead of 52 for ragged ones: a row's two
+// workgroups share their CUs with shorter rows'.
+//
+// What bounds it: instruction issue. A SIMD issues one instruction of its two waves
+// every five cycles or so (a sub-tile is about 150, 12 to 16 of them MFMAs of 32 or 64
+// cycles), and under full load the clock falls from 2.4 to 2.0 GHz.
+template <int FMT, int D, bool UNI>
+__global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a) {
+  constexpr int KT = 64, NS = 4, NI = 2;           // keys per stage, stages, waves that issue the DMA
   constexpr int NKK = D / 16, NDT = D / 32, NC = D / 16, NCB = D / 8;
   constexpr int TILE = KT * D, STAGE = 2 * TILE;   // bytes: K tile, then V tile
   constexpr int RPB = 1024 / D;                    // rows per 1 KiB DMA block
@@ -642,10 +638,7 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
   constexpr int PB = 2 * RPI + 1;                  // DMA instructions per stage and issuing wave
   constexpr int SCB = 2 * KT * 4;                  // bytes of a stage's scales
   static_assert(KT / RPB % NI == 0, "issuing waves split a tile evenly");
-  constexpr bool COOP = SH::COOP;
-  constexpr int WV = COOP ? KT * D * 2 : 0;        // bytes of a widened V tile
-  // stages, their scales, two widened V tiles
-  __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB + 2 * WV];
+  __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const QItem it = a.items[blockIdx.x];
@@ -671,7 +664,7 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
     const int vb = v0 + u * KT;
     const uint32_t sbase = ring_lds + (uint32_t)(slot * STAGE + w * 1024);
     const uint32_t ssc = ring_lds + (uint32_t)(NS * STAGE + slot * SCB + (w & 1) * KT * 4);
-    const float* sp = w & 1 ? keys.vs : keys.ks;   // scales by key: K's, then V's; of four waves two fetch the same
+    const float* sp = w & 1 ? keys.vs : keys.ks;   // scales by key: K's, then V's
     if (keys.whole(vb, KT)) {
       const int64_t at = (int64_t)keys.cell(vb) * D;
 #pragma unroll
@@ -778,40 +771,12 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt)
     voff[dt] = TILE + vrow * D + (((2 * dt + (q16 & 1)) ^ swz8<D>(vrow)) * 16) + 8 * (j16 & 1);
-  // the same of a widened V tile (rows 16 apart alike)
-  int woff[NDT][2];
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2) {
-      const int row = 8 * h2 + 4 * (q16 >> 1) + (j16 >> 2), x = 32 * dt + 16 * (q16 & 1) + 4 * (j16 & 3);
-      woff[dt][h2] = NS * STAGE + NS * SCB + row * D * 2 + (((x >> 3) ^ swz16<D>(row)) * 16) + (x & 7) * 2;
-    }
-  // K codes of operand i; the V operand of MFMA i (widened in place without COOP)
+  // K codes of operand i, V codes of MFMA i
   auto kraw = [&](int slot, int half, int i) {
     return *reinterpret_cast<const i32x4_t*>(ring + koff[i] + slot * STAGE + half * 32 * D);
   };
   auto vraw = [&](int slot, int half, int i) {
     return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(ring + voff[i % NDT] + slot * STAGE + (2 * half + i / NDT) * 16 * D));
-  };
-  auto vwide = [&](int slot, int half, int i) {
-    const uint8_t* p = ring + (slot & 1) * WV + (2 * half + i / NDT) * 32 * D;
-    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + woff[i % NDT][0]));
-    const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + woff[i % NDT][1]));
-    return (bf16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  // COOP: issuing wave w widens its share of the tile in `slot`, UN units (row, 16
-  // features) a lane, NI * RPB rows apart: the codes lie where its DMA put them
-  constexpr int UN = COOP ? KT / RPB / NI : 0;
-  const int ch0 = 2 * (lane % NC), wide0 = NS * STAGE + NS * SCB + row0 * D * 2 + ((ch0 ^ swz16<D>(row0)) * 16);
-  auto widen_tile = [&](int slot) {
-#pragma unroll
-    for (int x = 0; x < UN; ++x) {
-      const v4u y = *reinterpret_cast<const v4u*>(ring + lane_off + (slot * STAGE + TILE + x * NI * 1024));
-      uint8_t* to = ring + ((slot & 1) * WV + x * NI * 2048);
-      *reinterpret_cast<bf16x8_t*>(to + wide0) = widen8<FMT>(y[0], y[1]);
-      *reinterpret_cast<bf16x8_t*>(to + (wide0 ^ 16)) = widen8<FMT>(y[2], y[3]);
-    }
   };
   auto scales = [&](int slot, int half) { return reinterpret_cast<const float*>(ring + NS * STAGE + slot * SCB) + half * 32; };
   // x is computed here: keeps the compiler from sinking it past a fence
@@ -833,7 +798,7 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
   acc_t sA, sB;
   i32x4_t rk[D / 32];                                // K codes of a sub-tile
   i32x2_t rv[4];                                     // V codes read three MFMAs ahead
-  bf16x8_t fr[4];                                    // V operands: widened one MFMA ahead, or read three ahead
+  bf16x8_t fr[2];                                    // V operands, widened one MFMA ahead
   float kf = 0.0f, vs = 0.0f;                        // UNI: scales of the sub-tile whose scores are in
   auto score_mfma = [&](int i, acc_t& s) {
     if (i == 0) {
@@ -862,13 +827,11 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
   // of u - 1; writes the scores of u + 1 to sn and the weights of u to col.pp. Slots
   // of one MFMA each, in an order fixed by scheduling fences: P V of u - 1 (none for
   // the first sub-tile), then the scores of u + 1 (of stale LDS contents, and
-  // discarded, for the last); beside them the softmax of u in 16 steps, for a wave's
-  // MFMAs overlap its own VALU work only. With COOP the V operands of an odd
-  // sub-tile's P V are written before the barrier that opens it, so its first steps
-  // stand before its first MFMA, while they are read.
+  // discarded, for the last); beside them the widening of V's operands and the softmax
+  // of u in 16 steps, for a wave's MFMAs overlap its own VALU work only.
   auto sub_tile = [&](auto S, auto half_tag, auto first_tag, int u, acc_t& ss, acc_t& sn) {
     constexpr int H = decltype(half_tag)::value;
-    constexpr bool FIRST = decltype(first_tag)::value != 0, LATE = COOP && H == 1 && !FIRST;
+    constexpr bool FIRST = decltype(first_tag)::value != 0;
     const int s0 = S, sp = H ? s0 : (s0 + NS - 1) % NS, sx = H ? (s0 + 1) % NS : s0;
     if constexpr (H == 1) {
       // the next tile has landed once only later ones are in flight; past the barrier
@@ -877,12 +840,6 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
       wait_stages(min(t == 0 ? 2 : 1, max(ntiles - 2 - t, 0)));
       barrier();
       if (t + 3 < ntiles && t > 0) issue(t + 3, (s0 + NS - 1) % NS);
-      if constexpr (LATE) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) fr[i] = vwide(sp, 1 - H, i);
-      }
-    } else if constexpr (COOP) {
-      if (issuer) widen_tile(s0);
     }
     const int vb = v0 + u * 32;
     f32x4_t k4[4], v4[4];                            // scales by key: V's are read as they are needed
@@ -957,44 +914,33 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
         if (UNI && e >= 2) sum = add_pair(e / 2 - 1, sum);
       }
     };
-    constexpr int LEAD = LATE ? 4 : 0;               // steps before the first MFMA
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int st = 0; st < LEAD; ++st) step(st);
-    if (LEAD) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < NSL; ++i) {
       // operands: V's three MFMAs ahead (past the end: of the next sub-tile's P V), K's
       // beside the last MFMAs of P V
       const int jv = i + 3;
-      if constexpr (COOP) {
-        if (jv >= NSL ? H == 1 : jv < NPV && !FIRST)
-          fr[(jv >= NSL ? jv - NSL : jv) & 3] = jv >= NSL ? vwide(s0, H, jv - NSL) : vwide(sp, 1 - H, jv);
-      } else {
-        if (jv >= NSL)
-          rv[(jv - NSL) & 3] = vraw(s0, H, jv - NSL);
-        else if (jv < NPV && !FIRST)
-          rv[jv & 3] = vraw(sp, 1 - H, jv);
-      }
+      if (jv >= NSL)
+        rv[(jv - NSL) & 3] = vraw(s0, H, jv - NSL);
+      else if (jv < NPV && !FIRST)
+        rv[jv & 3] = vraw(sp, 1 - H, jv);
       if (i < NPV && i >= NPV - D / 32) rk[i - (NPV - D / 32)] = kraw(sx, 1 - H, i - (NPV - D / 32));
       if (i < NPV) {
         if constexpr (!FIRST)
-          col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[COOP ? i & 3 : i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
+          col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
       } else {
         score_mfma(i - NPV, sn);
       }
-      if constexpr (!COOP) {
-        // widen the next MFMA's operand (past the end: the next sub-tile's first)
-        if (i + 1 < NPV ? !FIRST : i + 1 == NSL) {
-          const i32x2_t& x = rv[i + 1 == NSL ? 0 : (i + 1) & 3];
-          fr[i + 1 == NSL ? 0 : (i + 1) & 1] = widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]);
-        }
+      // widen the next MFMA's operand (past the end: the next sub-tile's first)
+      if (i + 1 < NPV ? !FIRST : i + 1 == NSL) {
+        const i32x2_t& x = rv[i + 1 == NSL ? 0 : (i + 1) & 3];
+        fr[i + 1 == NSL ? 0 : (i + 1) & 1] = widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]);
       }
       // the softmax: steps 0 .. 7 beside P V, 8 .. 15 beside the scores
       const int b0 = i < NPV ? i * 8 / NPV : 8 + (i - NPV) * 8 / NSC, b1 = i < NPV ? (i + 1) * 8 / NPV : 8 + (i + 1 - NPV) * 8 / NSC;
 #pragma unroll
       for (int st = b0; st < b1; ++st)
-        if (st >= LEAD) step(st);
+        step(st);
       __builtin_amdgcn_sched_barrier(0);
       if (!FIRST && i == NPV - 1 && resc) {               // after P V of u - 1, before that of u
 #pragma unroll
@@ -1020,7 +966,6 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
     wait_stages(min(NS - 2, ntiles - 1));
     barrier();
     if (3 < ntiles) issue(3, 3);
-    if (COOP && u0 == 1 && issuer) widen_tile(0);
     // scores of the first sub-tile
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) rk[i] = kraw(0, u0, i);
@@ -1059,19 +1004,12 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
     }
     // P V of the last sub-tile
     const int ul = nsub - 1, sl = (ul >> 1) % NS, hl = ul & 1;
-    if constexpr (COOP) {
-      barrier();                                         // its tile may have been widened just now
+    // its first operand is widened, the next two are read
 #pragma unroll
-      for (int i = 0; i < NPV; ++i)
-        col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vwide(sl, hl, i), col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
-    } else {
-      // its first operand is widened, the next two are read
-#pragma unroll
-      for (int i = 0; i < NPV; ++i) {
-        if (i + 3 < NPV) rv[(i + 3) & 3] = vraw(sl, hl, i + 3);
-        col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
-        if (i + 1 < NPV) fr[(i + 1) & 1] = widen8<FMT>((uint32_t)rv[(i + 1) & 3][0], (uint32_t)rv[(i + 1) & 3][1]);
-      }
+    for (int i = 0; i < NPV; ++i) {
+      if (i + 3 < NPV) rv[(i + 3) & 3] = vraw(sl, hl, i + 3);
+      col.o[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i & 1], col.pp[i / NDT], col.o[i % NDT], 0, 0, 0);
+      if (i + 1 < NPV) fr[(i + 1) & 1] = widen8<FMT>((uint32_t)rv[(i + 1) & 3][0], (uint32_t)rv[(i + 1) & 3][1]);
     }
   }
 
@@ -1089,7 +1027,7 @@ __global__ __launch_bounds__(64 * MAXW, 2) void k_qattn_group(QAttnArgs a) {
     return;
   }
   barrier();                                   // the ring is read: each wave's share takes its rows
-  static_assert(MAXW * 32 * D * 2 <= NS * STAGE, "the row tiles fit the ring");
+  static_assert(kQRowTiles * 32 * D * 2 <= NS * STAGE, "the row tiles fit the ring");
   uint8_t* tile = ring + w * 32 * D * 2;
   const bool on = r < a.G * B;
   const float inv = 1.0f / col.lsum;
@@ -1156,10 +1094,8 @@ void attend(const QAttnArgs& a, hipStream_t s) {
   };
   auto by_groups = [&](auto uni_tag) {
     constexpr bool UNI = decltype(uni_tag)::value != 0;
-    if (a.RTW > 4)
-      go(k_qattn_group<FMT, D, 8, UNI>, a.RTW);
-    else if (a.RTW > 1)
-      go(k_qattn_group<FMT, D, 4, UNI>, a.RTW);
+    if (a.RTW > 1)
+      go(k_qattn_group<FMT, D, UNI>, a.RTW);
     else if (a.KS == 8)
       go(k_qattn_keys<FMT, D, 8, UNI>, 8);
     else if (a.KS == 4)
