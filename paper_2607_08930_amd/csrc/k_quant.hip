@@ -79,41 +79,40 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
   }
 }
 
-// Thread: 16 codes of one token.
+// Thread: as many codes of a token as fill 16 bytes read back, so that a wave's stores
+// are whole lines (16 codes a thread, stores of every other 16 bytes: 97 us instead of
+// XXX for 32 LLaDA-8B rows; two or four tokens a thread as well: 115).
 template <typename E, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_dequantize(DequantArgs a) {
-  constexpr int GS = D / 16;
+  constexpr int F = 16 / sizeof(E), GS = D / F;       // features per lane, lanes per token
   const bs_req_desc r = a.reqs[blockIdx.y];
   const int h = blockIdx.z >> 1, tensor = blockIdx.z & 1;
   const int u = blockIdx.x * 256 + threadIdx.x;
-  const int t = u / GS, col = (u % GS) * 16;
+  const int t = u / GS;
   if (t >= r.p + r.g) return;
-  const int64_t cell = (((int64_t)r.row * a.Hkv + h) * a.W + r.off + t) * D + col;
-  const float sc = (tensor ? a.v_scale : a.k_scale)[((int64_t)r.row * a.Hkv + h) * a.S + ((t + group_pad(r.p, a.lt)) >> a.lt)];
-  const v4u w = ld16((tensor ? a.v8 : a.k8) + cell);
-  E* out = static_cast<E*>(tensor ? a.v : a.k) + cell;
-  float y[16];
+  const int64_t row_head = (int64_t)r.row * a.Hkv + h, cell = (row_head * a.W + r.off + t) * D + u % GS * F;
+  const float sc = (tensor ? a.v_scale : a.k_scale)[row_head * a.S + ((t + group_pad(r.p, a.lt)) >> a.lt)];
+  const uint8_t* codes = (tensor ? a.v8 : a.k8) + cell;
+  uint32_t w[F / 4];
+  if constexpr (F == 8) {
+    const uint2 x = *reinterpret_cast<const uint2*>(codes);
+    w[0] = x.x;
+    w[1] = x.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(codes);
+  }
+  float y[F];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < F / 4; ++k) {
     float z[4];
     decode4<FMT>(w[k], z);
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[4 * k + e] = z[e] * sc;
   }
-  if constexpr (sizeof(E) == 2) {
+  v4u o;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      v4u o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = pack_bf16(y[8 * i + 2 * e], y[8 * i + 2 * e + 1]);
-      st16(out + 8 * i, o);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      st16(out + 4 * i, v4u{__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i + 2]),
-                            __float_as_uint(y[4 * i + 3])});
-  }
+  for (int e = 0; e < 4; ++e) o[e] = F == 8 ? pack_bf16(y[2 * e % F], y[(2 * e + 1) % F]) : __float_as_uint(y[e]);
+  st16(static_cast<E*>(tensor ? a.v : a.k) + cell, o);
 }
 
 template <typename E, int FMT, int D>
@@ -133,7 +132,8 @@ void quantize(const QuantArgs& a, int n, int max_len, hipStream_t s) {
 
 template <typename E, int FMT, int D>
 void dequantize(const DequantArgs& a, int n, int max_len, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)max_len * (D / 16) + 255) / 256), (unsigned)n, (unsigned)(2 * a.Hkv));
+  const int64_t lanes = (int64_t)max_len * (D * sizeof(E) / 16);
+  const dim3 grid((unsigned)((lanes + 255) / 256), (unsigned)n, (unsigned)(2 * a.Hkv));
   hipLaunchKernelGGL((k_kv_dequantize<E, FMT, D>), grid, dim3(256), 0, s, a);
 }
 
