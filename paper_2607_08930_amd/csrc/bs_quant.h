@@ -204,19 +204,17 @@ __device__ inline void group_tops(float (&top)[RP], int lt) {
     }
 }
 
-// 16 numbers, x(e), as codes in units of m / Q
-template <int FMT, class X>
-__device__ inline v4u encode16(float m, X x) {
+// 4 N numbers, x(e), as codes in units of m / Q
+template <int FMT, int N, class X>
+__device__ inline void encode(float m, X x, uint32_t (&w)[N]) {
   // x * (Q / m) is rounded by itself, not within the addition that rounds it to an integer
 #pragma clang fp contract(off)
   const float inv = quant_max<FMT>() / m;
-  v4u w;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < N; ++k) {
     const float y[4] = {x(4 * k) * inv, x(4 * k + 1) * inv, x(4 * k + 2) * inv, x(4 * k + 3) * inv};
     w[k] = encode4<FMT>(y);
   }
-  return w;
 }
 
 typedef __bf16 qb2 __attribute__((ext_vector_type(2)));

@@ -8,38 +8,20 @@
 // rounding before the code's own.
 //
 // Both directions are bound by HBM: each element is read once and written
-// once. A wave takes 64 / (D / 16) tokens at a time, 16 features a lane, so that
-// codes are stored and loaded as 16 bytes a lane and a wave's run is contiguous.
+// once.
 #include "bs_quant.h"
 
 namespace bs {
 namespace {
 
-// 16 consecutive elements of a lane, held as loaded
-template <typename E>
-struct Sixteen {
-  static constexpr int NV = sizeof(E);   // 16-byte vectors: 2 (bf16) or 4 (fp32)
-  v4u x[NV];
-  __device__ void load(const E* p) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) x[i] = ld16(reinterpret_cast<const char*>(p) + 16 * i);
-  }
-  __device__ float get(int e) const {
-    if constexpr (sizeof(E) == 2) {
-      const uint32_t w = x[e >> 3][(e >> 1) & 3];
-      return e & 1 ? bf_hi(w) : bf_lo(w);
-    } else {
-      return __uint_as_float(x[e >> 2][e & 3]);
-    }
-  }
-};
-
-// One wave quantises RS * RP tokens (a multiple of T) of one head of K or V.
+// One wave quantises RS * RP tokens (a multiple of T) of one head of K or V, a lane as
+// many features as fill 16 bytes, so that its loads are whole lines.
 template <typename E, int FMT, int D, int RP>
 __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
-  constexpr int GS = D / 16;        // lanes per token
-  constexpr int RS = 64 / GS;       // tokens per step
-  constexpr int CT = RS * RP;       // tokens per wave
+  constexpr int F = 16 / sizeof(E);   // features per lane
+  constexpr int GS = D / F;           // lanes per token
+  constexpr int RS = 64 / GS;         // tokens per step
+  constexpr int CT = RS * RP;         // tokens per wave
   const bs_req_desc r = a.reqs[blockIdx.y];
   const int h = blockIdx.z >> 1, tensor = blockIdx.z & 1;
   const int lane = threadIdx.x & 63, T = 1 << a.lt;
@@ -47,35 +29,44 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
   // virtual token v = t + pad: group v >> lt
   const int v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * CT;
   if (v0 >= len + pad) return;
-  const int64_t cell0 = (((int64_t)r.row * a.Hkv + h) * a.W + r.off) * D + (lane % GS) * 16;
+  const int64_t cell0 = (((int64_t)r.row * a.Hkv + h) * a.W + r.off) * D + (lane % GS) * F;
   const E* src = static_cast<const E*>(tensor ? a.v : a.k) + cell0;
 
-  Sixteen<E> x[RP];
+  v4u x[RP];
   float top[RP];
-  bool ok[RP];
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
     const int t = v0 + i * RS + lane / GS - pad;
-    ok[i] = t >= 0 && t < len;
-    if (ok[i]) x[i].load(src + (int64_t)t * D);
+    x[i] = v4u{0, 0, 0, 0};           // a token outside the row: no maximum, and not stored
+    if (t >= 0 && t < len) x[i] = ld16(src + (int64_t)t * D);
   }
+  auto get = [&](int i, int e) {
+    if constexpr (F == 8)
+      return e & 1 ? bf_hi(x[i][e >> 1]) : bf_lo(x[i][e >> 1]);
+    else
+      return __uint_as_float(x[i][e]);
+  };
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
     top[i] = 0.0f;
-    if (ok[i]) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top[i] = fmaxf(top[i], fabsf(x[i].get(e)));
-    }
+    for (int e = 0; e < F; ++e) top[i] = fmaxf(top[i], fabsf(get(i, e)));
   }
   group_tops<GS>(top, a.lt);
   uint8_t* codes = (tensor ? a.v8 : a.k8) + cell0;
   float* scales = (tensor ? a.v_scale : a.k_scale) + ((int64_t)r.row * a.Hkv + h) * a.S;
 #pragma unroll
   for (int i = 0; i < RP; ++i) {
-    const int v = v0 + i * RS + lane / GS;
+    const int v = v0 + i * RS + lane / GS, t = v - pad;
     const float m = fmaxf(top[i], kQuantFloor);
     if (lane % GS == 0 && (v & (T - 1)) == 0 && v < len + pad) scales[v >> a.lt] = m / quant_max<FMT>();
-    if (ok[i]) st16(codes + (int64_t)(v - pad) * D, encode16<FMT>(m, [&](int e) { return x[i].get(e); }));
+    if (t < 0 || t >= len) continue;
+    uint32_t w[F / 4];
+    encode<FMT, F / 4>(m, [&](int e) { return get(i, e); }, w);
+    if constexpr (F == 8)
+      *reinterpret_cast<uint2*>(codes + (int64_t)t * D) = uint2{w[0], w[1]};
+    else
+      *reinterpret_cast<uint32_t*>(codes + (int64_t)t * D) = w[0];
   }
 }
 
@@ -117,17 +108,20 @@ __global__ __launch_bounds__(256) void k_kv_dequantize(DequantArgs a) {
 
 template <typename E, int FMT, int D>
 void quantize(const QuantArgs& a, int n, int max_len, hipStream_t s) {
-  constexpr int RS = 64 / (D / 16);
+  constexpr int RS = 64 / (D * (int)sizeof(E) / 16);
   const int T = 1 << a.lt;
   auto go = [&](auto kernel, int rp) {
     const int per = 4 * RS * rp;    // tokens per workgroup
     const dim3 grid((unsigned)((max_len + T - 1 + per - 1) / per), (unsigned)n, (unsigned)(2 * a.Hkv));
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   };
-  if (T > 4 * RS)
-    go(k_kv_quantize<E, FMT, D, 8>, 8);
+  // eight loads in flight a lane, more where a group needs them
+  if (T > 16 * RS)
+    go(k_kv_quantize<E, FMT, D, 32>, 32);
+  else if (T > 8 * RS)
+    go(k_kv_quantize<E, FMT, D, 16>, 16);
   else
-    go(k_kv_quantize<E, FMT, D, 4>, 4);
+    go(k_kv_quantize<E, FMT, D, 8>, 8);
 }
 
 template <typename E, int FMT, int D>

@@ -130,10 +130,12 @@ __device__ inline void store_block(const QAttnArgs& a, const QItem& it, int c, i
     const float m = fmaxf(top[p], kQuantFloor);
     if (col == 0 && (r & (T - 1)) == 0) scales[r >> a.lt] = m / quant_max<FMT>();
     const v4u x[2] = {row(p, 0), row(p, 1)};
-    st16(codes + (int64_t)r * D, encode16<FMT>(m, [&](int e) {
-           const uint32_t y = x[e >> 3][(e >> 1) & 3];
-           return e & 1 ? bf_hi(y) : bf_lo(y);
-         }));
+    uint32_t y[4];
+    encode<FMT, 4>(m, [&](int e) {
+      const uint32_t z = x[e >> 3][(e >> 1) & 3];
+      return e & 1 ? bf_hi(z) : bf_lo(z);
+    }, y);
+    st16(codes + (int64_t)r * D, v4u{y[0], y[1], y[2], y[3]});
   }
 }
 
