@@ -71,12 +71,12 @@ hipError_t launch_kv_dequantize(const DequantArgs& a, bs_dtype dt, bs_qformat fm
 // of T <= 64 tokens and 64-key tiles then share borders. v0 and v1 are multiples of
 // 64, but for v1 = nv of the last piece.
 struct QItem {
-  int32_t req, kvh, rt0;     // request, KV head, first row tile
-  int32_t row, off, s, B;
-  int32_t pad, nv, v0, v1;
+  int32_t req;               // request
+  int32_t row, off, s;
+  int32_t nv, v0, v1;
   int32_t part;              // partial slot of a split row, or -1
-  int32_t fresh;
-  int32_t pad_[3];
+  uint16_t kvh, rt0;         // KV head, first row tile
+  uint8_t B, pad, fresh, pad_;
 };
 
 struct QMerge {

@@ -925,8 +925,8 @@ QRows qattn_rows(int L, int Hq, int Hkv) {
 QItem qattn_row(const bs_req_desc& r, int i, int L) {
   const Geo geo = geo_of(r, L);
   QItem it{};
-  it.req = i; it.row = r.row; it.off = r.off; it.s = geo.s; it.B = geo.B;
-  it.pad = group_pad(r.p, 6);
+  it.req = i; it.row = r.row; it.off = r.off; it.s = geo.s; it.B = (uint8_t)geo.B;   // L <= 64
+  it.pad = (uint8_t)group_pad(r.p, 6);
   it.nv = geo.len > geo.B ? it.pad + geo.len - geo.B : 0;
   it.v1 = it.nv;
   it.part = -1;
@@ -950,54 +950,67 @@ struct QPlan {
 // 1536: 72.3 / 56.8 / 56.5.
 int qattn_waves(size_t items) { return items <= 256 ? 8 : items <= 512 ? 4 : 2; }
 
-// One row tile: the time of a launch of `items` pieces, the longest of `longest`
-// tiles, `total` in all, in us at D = 128. A tile passes through a workgroup in
-// 0.42 us with eight waves (0.78 with four, 1.45 with two: its ring's bytes over the
-// memory's latency), through the whole machine in 3.15 ns (16 KiB at 5.2 TB/s), and the
-// two bounds meet gradually. Beside them 5 us to start and end, 5 for a merge launch and
-// 4 ns a partial. Against 60 measured launches (1 to 48 LLaDA-8B requests, 1 to 40
-// single-token batches of 2512 to 8512 keys, 1 to 4 rows of 8256 and 16256; whole and
-// in pieces of 2 to 48 tiles) within 15%.
-double qattn_estimate(size_t items, int longest, double total, int parts, int ks) {
-  const double c = ks == 8 ? 0.42 : ks == 4 ? 0.78 : 1.45;
-  const size_t slots = (size_t)kPlanCUs * 8 / ks;
+// The time of a launch, in us at D = 128: `fixed` to start and end, the longest piece
+// (a tile passes through a workgroup alone in `tile` us) and the whole list (`machine`
+// us a tile over all CUs), which meet gradually, and for a cut list a merge launch and
+// `part` us for each wave's partial. `slots` workgroups run at once.
+struct QCost {
+  double fixed, tile, machine, part;
+  size_t slots;
+};
+
+// One row tile: eight waves a CU in workgroups of ks, bound by the ring's bytes over the
+// memory's latency (16 KiB a tile), and by 5.2 TB/s in all. Against 60 measured
+// launches (1 to 48 LLaDA-8B requests, 1 to 40 single-token batches of 2512 to 8512 keys,
+// 1 to 4 rows of 8256 and 16256; whole and in pieces of 2 to 48 tiles) within 15%.
+// Several: two workgroups a CU, bound by instruction issue. Against 120 measured
+// launches (1 to 96 Dream-7B requests with blocks of 32 and 8, rows of 8512 keys among
+// them, whole and in pieces of 3 to 64 tiles) within 20%.
+QCost qattn_cost(const QRows& q, int ks) {
+  if (q.per > 1) return QCost{6.0, 1.0, std::max(3.15e-3, 1.15e-3 * q.per), 7e-3, (size_t)2 * kPlanCUs};
+  return QCost{5.0, ks == 8 ? 0.42 : ks == 4 ? 0.78 : 1.45, 3.15e-3, 4e-3, (size_t)kPlanCUs * 8 / ks};
+}
+
+// `items` pieces, the longest of `longest` tiles, `total` in all, `parts` waves' partials
+double qattn_estimate(const QCost& c, size_t items, int longest, double total, int parts) {
   // past one round a workgroup's place takes its share of the tiles, then half a piece more
-  const double run = items <= slots ? longest : std::max((double)longest, total / slots + 0.5 * total / items);
-  return 5.0 + std::hypot(c * run, 3.15e-3 * total) + (parts ? 5.0 + 4e-3 * parts : 0.0);
+  const double run = items <= c.slots ? longest : std::max((double)longest, total / c.slots + 0.5 * total / items);
+  return c.fixed + std::hypot(c.tile * run, c.machine * total) + (parts ? 5.0 + c.part * parts : 0.0);
 }
 
 QPlan qattn_plan(const bs_req_desc* reqs, int n, int L, int Hkv, const QRows& q) {
   std::vector<Run> runs((size_t)n);
-  for (int i = 0; i < n; ++i) runs[i] = Run{qattn_tiles(qattn_row(reqs[i], i, L)), Hkv * q.groups};
-  if (q.per > 1) return QPlan{split_cap(runs, PlanShape{1, 1.3, kMergePerPartShared}), 0};
   int longest = 0;
   double total = 0.0;
-  for (const Run& r : runs) {
-    longest = std::max(longest, r.tiles);
-    total += (double)r.tiles * r.count;
+  for (int i = 0; i < n; ++i) {
+    runs[i] = Run{qattn_tiles(qattn_row(reqs[i], i, L)), Hkv * q.groups};
+    longest = std::max(longest, runs[i].tiles);
+    total += (double)runs[i].tiles * runs[i].count;
   }
-  const size_t rows = (size_t)n * Hkv;
-  QPlan best{0, qattn_waves(rows)};
-  double least = qattn_estimate(rows, longest, total, 0, best.ks);
+  const size_t rows = (size_t)n * Hkv * q.groups;
+  QPlan best{0, q.per > 1 ? 0 : qattn_waves(rows)};
+  double least = qattn_estimate(qattn_cost(q, best.ks), rows, longest, total, 0);
   for (int ks : {8, 4, 2}) {
-    const size_t slots = (size_t)kPlanCUs * 8 / ks;
-    // from an even share of the tiles upwards; the first cap whose pieces fit one round ends it
-    for (int cap = std::max(2, (int)std::ceil(total / slots)); cap < longest; cap += std::max(1, cap / 8)) {
+    const QCost cost = qattn_cost(q, ks);
+    // from an even share of the tiles upwards; with one row tile the first cap whose pieces
+    // fit one round ends it (few row tiles write few partials)
+    for (int cap = std::max(2, (int)std::ceil(total / cost.slots)); cap < longest; cap += std::max(1, cap / 8)) {
       size_t items = 0;
       int parts = 0, piece = 0;
       for (const Run& r : runs) {
         const int np = (r.tiles + cap - 1) / cap;
         items += (size_t)np * r.count;
-        if (np > 1) parts += np * r.count;
+        if (np > 1) parts += np * r.count * q.per;
         piece = std::max(piece, (r.tiles + np - 1) / np);
       }
-      const double t = qattn_estimate(items, piece, total, parts, ks);
+      const double t = qattn_estimate(cost, items, piece, total, parts);
       if (t < least) {
         least = t;
-        best = QPlan{cap, ks};
+        best = QPlan{cap, q.per > 1 ? 0 : ks};
       }
-      if (items <= slots) break;
+      if (q.per == 1 && items <= cost.slots) break;
     }
+    if (q.per > 1) break;      // no choice of ks
   }
   return best;
 }
@@ -1011,43 +1024,44 @@ void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int H
   const QRows q = qattn_rows(L, Hq, Hkv);
   const QPlan plan = split ? qattn_plan(reqs, n, L, Hkv, q) : QPlan{0, qattn_waves((size_t)n * Hkv)};
   const int cap = plan.cap;
+  // a request's pieces are alike for all its heads: cut and sort one head's
   std::vector<QItem> pieces, rows((size_t)n);
   std::vector<QMerge> merges;
+  pieces.reserve((size_t)n);
   int parts = 0;
   for (int i = 0; i < n; ++i) {
     const QItem row = rows[i] = qattn_row(reqs[i], i, L);
     const int nt = qattn_tiles(row), np = cap > 0 && nt > cap ? (nt + cap - 1) / cap : 1;
-    for (int h = 0; h < Hkv; ++h) {
-      // the pieces of a row's first workgroup take np partial slots, then those of its second, ...
-      if (np > 1)
-        for (int gr = 0; gr < q.groups; ++gr) merges.push_back(QMerge{i, h, gr * q.per, row.B, parts + gr * np, np, {0, 0}});
-      for (int k = 0; k < np; ++k) {
-        QItem it = row;
-        it.kvh = h;
-        if (np > 1) {
-          it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
-          it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
-          it.part = parts + k;
-          it.fresh = k == 0;
-        }
-        pieces.push_back(it);
+    for (int k = 0; k < np; ++k) {
+      QItem it = row;
+      if (np > 1) {
+        it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
+        it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
+        it.part = parts + k;         // of the first head's first workgroup; the others' follow, np apart
+        it.fresh = k == 0;
       }
-      if (np > 1) parts += np * q.groups;
+      pieces.push_back(it);
     }
+    if (np > 1)
+      for (int h = 0; h < Hkv; ++h)
+        for (int gr = 0; gr < q.groups; ++gr, parts += np) merges.push_back(QMerge{i, h, gr * q.per, row.B, parts, np, {0, 0}});
   }
   // longest first; the workgroups of a piece, which read the same keys, stand eight
   // apart, which is the same XCD and its L2
   std::stable_sort(pieces.begin(), pieces.end(), [](const QItem& x, const QItem& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
   std::vector<QItem> items;
-  items.reserve(pieces.size() * q.groups);
-  for (size_t b = 0; b < pieces.size(); b += 8)
+  const size_t heads = pieces.size() * Hkv;
+  items.reserve(heads * q.groups);
+  for (size_t b = 0; b < heads; b += 8)
     for (int gr = 0; gr < q.groups; ++gr)
-      for (size_t k = b; k < std::min(b + 8, pieces.size()); ++k) {
-        QItem it = pieces[k];
-        it.rt0 = gr * q.per;
+      for (size_t k = b; k < std::min(b + 8, heads); ++k) {
+        QItem it = pieces[k / Hkv];
+        const int h = (int)(k % Hkv);
+        it.kvh = (uint16_t)h;
+        it.rt0 = (uint16_t)(gr * q.per);
         if (it.part >= 0) {
-          const int nt = qattn_tiles(rows[it.req]);
-          it.part += gr * ((nt + cap - 1) / cap);
+          const int nt = qattn_tiles(rows[it.req]), np = (nt + cap - 1) / cap;
+          it.part += (h * q.groups + gr) * np;
         }
         items.push_back(it);
       }
