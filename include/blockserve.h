@@ -373,8 +373,8 @@ int bs_kv_scale_groups(int p, int g, int T);
  * and no cell or scale outside the rows is written. Inputs are finite; a group
  * that holds an infinity or NaN gets codes and a scale of no meaning, others
  * are not affected. Supported: dt BS_BF16 or BS_F32, D in {64, 128},
- * n <= 65535, Hkv <= 32767, tensors 16-byte aligned (scales 4), codes disjoint
- * from k and v. The descriptors are validated as everywhere (L and k only there).
+ * n <= 65535, Hkv <= 32767, tensors 16-byte aligned (scales 4); codes and scales
+ * overlap neither k and v nor each other (BS_ERR_OVERLAP). The descriptors are validated as everywhere (L and k only there).
  */
 int bs_kv_quantize(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
                    bs_qformat fmt, int T, const void* k, const void* v, void* k8, void* v8, float* k_scale,
@@ -398,12 +398,15 @@ int bs_kv_dequantize(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, 
  * write_back != 0 also quantises rows j < B_i of k_new and v_new into the
  * block's cells and scales, exactly as bs_kv_quantize would from a box; the
  * cache is otherwise only read, and padding and the stale block slot never are
- * (their scales neither). Sums and softmax statistics are fp32; queries and
- * codes meet as fp16 (queries scaled by a power of two for each row), weights are
- * rounded to fp16 for the codes and to bf16 for the block's own values.
+ * (their scales neither). Sums and softmax statistics are fp32, weights are
+ * rounded to bf16. Up to 32 query rows a KV head (L * Hq / Hkv), products of
+ * queries and codes are exact. Beyond, a query element meets the codes as a number
+ * of theirs plus another: off by at most 2^-17 (BS_E4M3) or 2^-15 (BS_I8) of the
+ * largest element of its row and head, which is less than the input's own rounding
+ * of that element. The block's own keys always meet the queries as given.
  * Scales must be positive and finite, within 2^-80 .. 2^80.
  * Supported: D in {64, 128}, L <= 64, Hq / Hkv <= 8, T a divisor of L,
- * W * D < 2^31; tensors 16-byte aligned (scales 4).
+ * n * Hkv <= 2^20, W * D < 2^31; tensors 16-byte aligned (scales 4), ws too.
  * ws: NULL or a workspace of ws_bytes bytes (contents on entry ignored). With
  * at least bs_quant_attention_workspace_bytes(...) bytes, long rows are split
  * over workgroups and joined by a second launch, as for

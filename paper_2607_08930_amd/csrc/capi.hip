@@ -10,6 +10,7 @@
 #include <functional>
 #include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -906,6 +907,22 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// whether any two of these byte ranges meet, at least one of them `out`
+struct Range {
+  const void* p;
+  int64_t n;
+  bool out;
+};
+bool any_overlap(std::initializer_list<Range> r) {
+  for (const Range* a = r.begin(); a != r.end(); ++a)
+    for (const Range* b = a + 1; b != r.end(); ++b)
+      if ((a->out || b->out) && overlap(a->p, a->n, b->p, b->n)) return true;
+  return false;
+}
+
+// the host has no memory for a call's lists: nothing was enqueued
+int no_memory(bs_ctx* c) { return fail(c, BS_ERR_UNSUPPORTED, "no host memory for the call's lists"); }
+
 // ---- 8-bit attention plan
 // Row tiles of 32 query rows (j G + h') per KV head and per workgroup: up to
 // kQRowTiles waves a workgroup, the tiles of a head spread evenly over as few of
@@ -913,6 +930,10 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 struct QRows {
   int tiles, groups, per;   // row tiles of a head, workgroups, row tiles per workgroup
 };
+
+// requests times KV heads of one call: bounds the work list (at most four workgroups
+// for each and a round of pieces, 40 bytes) and every index made from it
+constexpr int kMaxQRows = 1 << 20;
 
 QRows qattn_rows(int L, int Hq, int Hkv) {
   QRows q;
@@ -1533,7 +1554,7 @@ int bs_kv_scale_groups(int p, int g, int T) {
 
 int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
                    bs_qformat fmt, int T, const void* k, const void* v, void* k8, void* v8, float* k_scale,
-                   float* v_scale, int S, void* stream) {
+                   float* v_scale, int S, void* stream) try {
   int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
   if (st) return st;
   if (!dtype_bytes(dt)) return fail(c, BS_ERR_INVALID_ARG, "bad dtype %d", (int)dt);
@@ -1543,9 +1564,9 @@ int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int 
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16))
     return fail(c, BS_ERR_INVALID_ARG, "k and v must be non-NULL and 16-byte aligned");
   const int64_t cells = (int64_t)R * Hkv * W * D, xb = cells * dtype_bytes(dt);
-  if (overlap(k, xb, k8, cells) || overlap(k, xb, v8, cells) || overlap(v, xb, k8, cells) || overlap(v, xb, v8, cells) ||
-      overlap(k8, cells, v8, cells))
-    return fail(c, BS_ERR_OVERLAP, "the codes overlap k, v or each other");
+  const int64_t sb = (int64_t)R * Hkv * S * 4;
+  if (any_overlap({{k, xb, false}, {v, xb, false}, {k8, cells, true}, {v8, cells, true}, {k_scale, sb, true}, {v_scale, sb, true}}))
+    return fail(c, BS_ERR_OVERLAP, "codes or scales overlap k, v or each other");
   DeviceGuard dg(c->device);
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1559,11 +1580,13 @@ int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int 
   a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
   a.k_scale = k_scale; a.v_scale = v_scale;
   return end(c, call, s, launch_kv_quantize(a, dt, fmt, D, n, longest_row(reqs, n), s), "quantize launch");
+} catch (const std::bad_alloc&) {
+  return no_memory(c);
 }
 
 int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int Hkv, int D, bs_dtype dt,
                      bs_qformat fmt, int T, const void* k8, const void* v8, const float* k_scale,
-                     const float* v_scale, int S, void* k, void* v, void* stream) {
+                     const float* v_scale, int S, void* k, void* v, void* stream) try {
   int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
   if (st) return st;
   if (!dtype_bytes(dt)) return fail(c, BS_ERR_INVALID_ARG, "bad dtype %d", (int)dt);
@@ -1573,9 +1596,9 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16))
     return fail(c, BS_ERR_INVALID_ARG, "k and v must be non-NULL and 16-byte aligned");
   const int64_t cells = (int64_t)R * Hkv * W * D, xb = cells * dtype_bytes(dt);
-  if (overlap(k, xb, k8, cells) || overlap(k, xb, v8, cells) || overlap(v, xb, k8, cells) || overlap(v, xb, v8, cells) ||
-      overlap(k, xb, v, xb))
-    return fail(c, BS_ERR_OVERLAP, "k or v overlaps the codes or the other");
+  const int64_t sb = (int64_t)R * Hkv * S * 4;
+  if (any_overlap({{k, xb, true}, {v, xb, true}, {k8, cells, false}, {v8, cells, false}, {k_scale, sb, false}, {v_scale, sb, false}}))
+    return fail(c, BS_ERR_OVERLAP, "k or v overlaps the codes, the scales or the other");
   DeviceGuard dg(c->device);
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1589,10 +1612,17 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
   a.k_scale = k_scale; a.v_scale = v_scale;
   a.k = k; a.v = v;
   return end(c, call, s, launch_kv_dequantize(a, dt, fmt, D, n, longest_row(reqs, n), s), "dequantize launch");
+} catch (const std::bad_alloc&) {
+  return no_memory(c);
 }
 
-size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D) {
+size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D) try {
   if (!reqs || n <= 0 || L < 1 || L > 64 || Hkv < 1 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 8 || (D != 64 && D != 128)) return 0;
+  if ((int64_t)n * Hkv > kMaxQRows) return 0;
+  for (int i = 0; i < n; ++i) {
+    const bs_req_desc& r = reqs[i];
+    if (r.p < 0 || r.g < 1 || r.k < 0 || (int64_t)r.k * L >= r.g || (int64_t)r.p + r.g > INT32_MAX / 64) return 0;
+  }
   const QRows q = qattn_rows(L, Hq, Hkv);
   const int cap = qattn_plan(reqs, n, L, Hkv, q).cap;
   int parts = 0;
@@ -1602,13 +1632,15 @@ size_t bs_quant_attention_workspace_bytes(const bs_req_desc* reqs, int n, int L,
       if (nt > cap) parts += (nt + cap - 1) / cap * Hkv * q.groups;
     }
   return qattn_part_bytes(parts, q, D);
+} catch (const std::bad_alloc&) {
+  return 0;
 }
 
 int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, int D,
                                    bs_qformat fmt, int T, float scale, const void* q, const void* k_new,
                                    const void* v_new, void* k8, void* v8, float* k_scale, float* v_scale, int S,
                                    int R, int W, int write_back, void* out, void* ws, size_t ws_bytes,
-                                   void* stream) {
+                                   void* stream) try {
   int st = check_quant(c, reqs, n, L, R, W, Hkv, D, fmt, T, S);
   if (st) return st;
   if (Hq < 1 || Hq % Hkv) return fail(c, BS_ERR_UNSUPPORTED, "Hq=%d not a multiple of Hkv=%d", Hq, Hkv);
@@ -1616,7 +1648,7 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
     return fail(c, BS_ERR_UNSUPPORTED, "the 8-bit attention needs L <= 64 and Hq/Hkv <= 8 (L=%d, Hq/Hkv=%d)", L, Hq / Hkv);
   if (L % T) return fail(c, BS_ERR_UNSUPPORTED, "T=%d does not divide the block length L=%d", T, L);
   if (!(scale == scale)) return fail(c, BS_ERR_INVALID_ARG, "scale is NaN");
-  if ((int64_t)n * Hq * L > INT32_MAX) return fail(c, BS_ERR_UNSUPPORTED, "n * Hq * L exceeds the launch grid");
+  if ((int64_t)n * Hkv > kMaxQRows) return fail(c, BS_ERR_UNSUPPORTED, "n * Hkv exceeds %d", kMaxQRows);
   if (n == 0) return BS_OK;
   st = check_quant_tensors(c, k8, v8, k_scale, v_scale);
   if (st) return st;
@@ -1656,13 +1688,15 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   a.write_back = write_back ? 1 : 0;
   a.out = static_cast<uint16_t*>(out);
   return end(c, call, s, launch_qattn(a, fmt, s), "8-bit attention launch");
+} catch (const std::bad_alloc&) {
+  return no_memory(c);
 }
 
 // ------------------------------------------------------------------ norm and rotation
 int bs_qk_norm_rope(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int W, int whole_rows, int Hq, int Hkv,
                     int D, bs_dtype dt, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                     const void* q_weight, const void* k_weight, float eps, float rope_base, void* q_out,
-                    void* k_out, void* stream) {
+                    void* k_out, void* stream) try {
   if (!c) return fail(nullptr, BS_ERR_INVALID_ARG, "ctx is NULL");
   int st = check_reqs(c, reqs, n, L, R, W);
   if (st) return st;
@@ -1726,6 +1760,8 @@ int bs_qk_norm_rope(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int
   a.qw = q_weight; a.kw = k_weight;
   a.q_out = q_out; a.k_out = k_out;
   return end(c, call, s, launch_norm_rope(a, dt, n, max_tokens, s), "norm and rotation launch");
+} catch (const std::bad_alloc&) {
+  return no_memory(c);
 }
 
 // ------------------------------------------------------------------ fused step

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
 
 // Thread: as many codes of a token as fill 16 bytes read back, so that a wave's stores
 // are whole lines (16 codes a thread, stores of every other 16 bytes: 97 us instead of
-// XXX for 32 LLaDA-8B rows; two or four tokens a thread as well: 115).
+// 87 for 32 LLaDA-8B rows; two or four tokens a thread as well: 115).
 template <typename E, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_dequantize(DequantArgs a) {
   constexpr int F = 16 / sizeof(E), GS = D / F;       // features per lane, lanes per token

@@ -6,8 +6,8 @@
 //
 // Row tiles. The query rows of a KV head's group are counted r = j G + h' (block
 // row j, head h' of the group), so that short blocks of grouped heads fill the 32
-// columns of an MFMA; a wave owns 32 of them, a workgroup up to eight waves that
-// share the K/V tiles.
+// columns of an MFMA; a wave owns 32 of them, a workgroup of several row tiles up to
+// four waves that share the K/V tiles.
 //
 // Virtual keys. The cached keys (prefix and suffix without the active block) are
 // counted v = pad + 0, 1, ..., pad = -p mod 64. Block borders lie at multiples

@@ -4,13 +4,15 @@ the block, the per-head norm with rotation, and the four together.
 
 Tolerances. Codes, scales and numbers read back are chains of single fp32
 roundings that the oracle repeats, so they match bit for bit. Attention: the
-scores of codes are fp32 sums of exact products of fp16 numbers (a query element
-below 2^-14 of its row's largest loses at most 2^-25 of that), the weights are
-rounded to at most 2^-8 (bf16, the block's own keys; fp16 for the others) and the
-output to 2^-8 of its value, so |d| <= 2^-8 |out| + (2^-8 + 2^-9) spread with the
-spread of oracle.quant; 2^-9 covers the fp32 scores: their error e moves a weight
-by the factor exp(e), and e <= 128 * 2^-24 * sum |q k| stays under 2^-10 for the
-sum |q k| scale <= 128 that the inputs keep (checked), as does the hardware exp2.
+scores are fp32 sums of exact products, the weights are rounded to bf16 (2^-8) and
+the output to 2^-8 of its value, so |d| <= 2^-8 |out| + (2^-8 + 2^-9) spread with
+the spread of oracle.quant; 2^-9 covers the scores: their error e moves a weight by
+the factor exp(e). Of it, e <= 128 * 2^-24 * sum |q k| from the fp32 sums stays under
+2^-10 for the sum |q k| scale <= 128 that the inputs keep, as does the hardware
+exp2. With more than 32 query rows a KV head a query element is off by up to 2^-17
+(e4m3) or 2^-15 (int8) of its row's largest, with either sign: over a key of
+deviation s that is a score error of deviation 2^-15 max|q| s / sqrt(3), 2^-14 s for
+the normal queries here, and it averages out over the keys of a row.
 Norm: fp32 sums of 256 squares at most, one reciprocal square root and two
 products (under 16 roundings of 2^-24) and an angle good to 2^-22 turns: 4e-6 of
 the rotated pair's size in all, then the output's rounding (2^-8 bf16, 2^-24
@@ -522,6 +524,32 @@ def test_refusals(ctx):
     bs.bs_kv_quantize(ctx, none, 32, 1, 1, 2, 128, bs.BS_BF16, 0, 32, None, None, None, None, None, None, 1)
     bs.bs_qk_norm_rope(ctx, none, 32, 1, 1, False, 4, 2, 128, bs.BS_BF16, None, 512, None, 256, None, None, 1e-6, 1e4, None, None)
     assert [bs.bs_kv_scale_groups(*a) for a in ((5, 6, 4), (0, 1, 64), (5, 6, 3), (-1, 2, 4), (3, 0, 4))] == [4, 1, 0, 0, 0]
+
+
+def test_refusals_of_overlaps_and_of_lists_too_long(ctx):
+    torch, bs, _ = lazy()
+    reqs = np.array([(5, 8, 0, 0, 0)], bs.REQ_DTYPE)
+    k, v, k8, v8 = (torch.zeros(16 * 128, dtype=t, device="cuda") for t in (torch.bfloat16, torch.bfloat16, torch.uint8, torch.uint8))
+    ks, vs = (torch.ones(8, device="cuda") for _ in range(2))
+    for name, a in (("k over scales", dict(ks=k)), ("codes over scales", dict(vs=k8)), ("one scale tensor", dict(vs=ks)),
+                    ("scales that meet", dict(vs=ks.data_ptr() + 16)), ("one code tensor", dict(v8=k8))):
+        x = dict(k=k, v=v, k8=k8, v8=v8, ks=ks, vs=vs)
+        x.update(a)
+        with pytest.raises(bs.BlockServeError, match="overlap") as e:
+            bs.bs_kv_quantize(ctx, reqs, 8, 1, 16, 1, 128, bs.BS_BF16, 0, 8, x["k"], x["v"], x["k8"], x["v8"], x["ks"], x["vs"], 8)
+        assert e.value.name == "BS_ERR_OVERLAP", name
+    for name, a in (("k over scales", dict(ks=k)), ("v over codes", dict(v8=v)), ("one box", dict(v=k))):
+        x = dict(k=k, v=v, k8=k8, v8=v8, ks=ks, vs=vs)
+        x.update(a)
+        with pytest.raises(bs.BlockServeError, match="overlap") as e:
+            bs.bs_kv_dequantize(ctx, reqs, 8, 1, 16, 1, 128, bs.BS_BF16, 0, 8, x["k8"], x["v8"], x["ks"], x["vs"], 8, x["k"], x["v"])
+        assert e.value.name == "BS_ERR_OVERLAP", name
+    many = np.zeros(64, bs.REQ_DTYPE)
+    many["p"], many["g"], many["row"] = 5, 8, np.arange(64)
+    with pytest.raises(bs.BlockServeError, match="n . Hkv") as e:
+        bs.bs_quant_cache_block_attention(ctx, many, 8, 20000, 20000, 64, 0, 8, 0.0, k, k, v, k8, v8, ks, vs, 8, 64, 16, True, k)
+    assert e.value.name == "BS_ERR_UNSUPPORTED"
+    assert bs.bs_quant_attention_workspace_bytes(many, 8, 20000, 20000, 64) == 0
 
 
 # ---------------------------------------------------------------- as a serving program uses them
