@@ -6,7 +6,9 @@ blocks' token ids and mask bits -> dual-cache block attention for each layer
 mask back into the dense box. ``run_step`` enqueues the whole step with one
 ``bs_mixed_state_step`` call (decode then reads and writes the dense boxes
 directly) or, with ``fused=False``, as the separate K1/K2/K3/K1^-1 calls. At a
-block boundary ``compact`` first rewrites the KV boxes of every layer.
+block boundary ``compact`` first rewrites the KV boxes of every layer. With a
+``QuantCache`` in the state the cache of every layer is held in 8 bits: attention
+and its write go there, layer by layer, ahead of the rest.
 PyTorch only provides device memory and the stream; every step runs in
 libblockserve's kernels.
 """
@@ -20,7 +22,8 @@ import torch
 from . import (BS_BF16, BS_F32, Context, bs_decode_workspace_bytes, bs_dual_cache_block_attention,
                bs_step_workspace_bytes,
                bs_gather_active_blocks_n, bs_kv_scatter_compact, bs_mixed_state_step, bs_parallel_decode,
-               bs_scatter_active_blocks_n)
+               bs_quant_attention_workspace_bytes, bs_scatter_active_blocks_n)
+from .quant_cache import QuantCache
 
 
 def dt_code(dtype: str) -> int:
@@ -49,7 +52,7 @@ class Layer:
     q: torch.Tensor        # [n][L][Hq][D]
     k_new: torch.Tensor    # [n][L][Hkv][D]
     v_new: torch.Tensor
-    k_cache: torch.Tensor  # [R][Hkv][W][D]
+    k_cache: torch.Tensor  # [R][Hkv][W][D]; None with an 8-bit cache
     v_cache: torch.Tensor
     out: torch.Tensor      # [n][L][Hq][D]
 
@@ -85,6 +88,7 @@ class StepState:
     dec_ws: torch.Tensor = None      # the step's workspace: the decode's, then the attention's partials
     ws_key: bytes = None             # descriptors dec_ws was last sized for
     flags_host: torch.Tensor = None
+    cache: QuantCache = None         # the layers' cache in 8 bits, in place of Layer.k_cache / v_cache
     extra: dict = field(default_factory=dict)
 
     def alloc(self):
@@ -107,7 +111,11 @@ class StepState:
         key = reqs.tobytes()
         if key != self.ws_key:
             dt = dt_code(self.dtype)
-            need = bs_step_workspace_bytes(reqs, self.L, self.Hq, self.Hkv, self.D, dt, self.V, dt)
+            if self.cache is None:
+                need = bs_step_workspace_bytes(reqs, self.L, self.Hq, self.Hkv, self.D, dt, self.V, dt)
+            else:      # one after the other: the attention's partials and the decode's share the room
+                need = max(bs_quant_attention_workspace_bytes(reqs, self.L, self.Hq, self.Hkv, self.D),
+                           bs_decode_workspace_bytes(len(reqs), self.L, self.V, dt))
             if need > self.dec_ws.numel():
                 self.dec_ws = torch.empty(need, dtype=torch.uint8, device=self.dec_ws.device)
             self.ws_key = key
@@ -127,6 +135,12 @@ def run_step(ctx: Context, st: StepState, reqs: np.ndarray, *, stream=None, want
     conf = st.conf if want_conf else None
     ws = st.workspace_for(reqs)
     ws_bytes = ws.numel() if split else bs_decode_workspace_bytes(len(reqs), L, st.V, dt)
+    if st.cache is not None:
+        for l, x in enumerate(lays):
+            st.cache.attend(ctx, reqs, l, x.q, x.k_new, x.v_new, x.out, Hq=st.Hq, scale=st.scale,
+                            write_back=st.write_back, ws=ws if split else None, ws_bytes=ws_bytes if split else 0,
+                            stream=stream)
+        lays = []
     if fused:
         bs_mixed_state_step(ctx, reqs, L, R, W,
                             [(x.q, x.k_new, x.v_new, x.k_cache, x.v_cache, x.out) for x in lays],
