@@ -274,7 +274,9 @@ int upload(bs_ctx* c, hipStream_t s, const Key& key, Make make, Slot** out) {
   }
   if (!sl.ready) {
     hipError_t e = hipEventCreateWithFlags(&sl.ready, hipEventDisableTiming);
-    if (e == hipSuccess) e = hipEventCreateWithFlags(&sl.done, hipEventDisableTiming);
+    // `done` only says that a slot is no longer read, so it needs no write-back of the
+    // caches to the host (1.9 us a call on the GPU)
+    if (e == hipSuccess) e = hipEventCreateWithFlags(&sl.done, hipEventDisableTiming | hipEventDisableSystemFence);
     if (e != hipSuccess) return hip_fail(c, e, "hipEventCreate");
   }
   std::memcpy(sl.h, blob.bytes.data(), n);
