@@ -19,6 +19,31 @@ __host__ __device__ inline int group_pad(int p, int lt) { return (int)(-(unsigne
 constexpr float kQuantFloor = 5.421010862427522e-20f;   // 2^-64
 constexpr float kE4m3Max = 448.0f, kI8Max = 127.0f;
 
+// Descriptors that travel in the kernel's arguments: lists of up to kNear entries need
+// no upload, no slot and no event, and the launch can be captured as it stands. A
+// launch takes up to 4 KiB of arguments.
+constexpr int kNear = 64;
+// Entry i (uniform) of a list in device memory, or of `near` in the kernel's arguments.
+// Both are constant memory to the launch, so the entry comes in scalar loads.
+template <class T>
+__device__ inline T list_entry(const T* far, const T* near, int i) {
+  static_assert(sizeof(T) % 4 == 0);
+  typedef const __attribute__((address_space(4))) uint32_t* cptr;
+  const cptr p = (cptr)(far ? far : near) + (int64_t)i * (sizeof(T) / 4);
+  union {
+    uint32_t w[sizeof(T) / 4];
+    T t;
+  } u;
+#pragma unroll
+  for (int k = 0; k < (int)(sizeof(T) / 4); ++k) u.w[k] = p[k];
+  return u.t;
+}
+struct ReqList {
+  const bs_req_desc* far;    // in device memory, or NULL: in `near`
+  bs_req_desc near[kNear];
+  __device__ bs_req_desc get(int i) const { return list_entry(far, near, i); }
+};
+
 struct NormRopeArgs {
   const bs_req_desc* reqs;
   const float2* freq;        // [D / 2]: turns per position of feature pair f, as high + low part
@@ -38,7 +63,7 @@ hipError_t launch_norm_rope(const NormRopeArgs& a, bs_dtype dt, int n, int max_t
 
 // Whole rows of the box: k, v [R][Hkv][W][D] of the call's type
 struct QuantArgs {
-  const bs_req_desc* reqs;
+  ReqList reqs;
   int Hkv, W, S, lt;
   const void* k;
   const void* v;
@@ -51,7 +76,7 @@ hipError_t launch_kv_quantize(const QuantArgs& a, bs_dtype dt, bs_qformat fmt, i
                               hipStream_t s);
 
 struct DequantArgs {
-  const bs_req_desc* reqs;
+  ReqList reqs;
   int Hkv, W, S, lt;
   const uint8_t* k8;
   const uint8_t* v8;
@@ -63,34 +88,35 @@ struct DequantArgs {
 hipError_t launch_kv_dequantize(const DequantArgs& a, bs_dtype dt, bs_qformat fmt, int D, int n, int max_len,
                                 hipStream_t s);
 
-// Attention work item: the row tiles of one (request, KV head) that one workgroup
-// serves, against the cached keys [v0, v1) of its piece in virtual keys (below) and,
-// where `fresh` is set, the block's own keys.
+// Attention work: a request's row, or a piece of it, for all heads alike: the cached
+// keys [v0, v1) in virtual keys (below) and, where `fresh` is set, the block's own keys.
 // Virtual keys count the cached keys without the active block from pad = -p mod 64:
 // v < s + pad is cell v - pad, v >= s + pad is cell v - pad + B; nv ends them. Groups
 // of T <= 64 tokens and 64-key tiles then share borders. v0 and v1 are multiples of
 // 64, but for v1 = nv of the last piece.
-struct QItem {
+struct QPiece {
   int32_t req;               // request
   int32_t row, off, s;
   int32_t nv, v0, v1;
-  int32_t part;              // partial slot of a split row, or -1
-  uint16_t kvh, rt0;         // KV head, first row tile
+  int32_t part;              // partial slot of a split row's first head and workgroup, or -1
+  int32_t np;                // pieces of the row
+  int32_t split;             // of entry m of the list: the first piece of the m-th split row
   uint8_t B, pad, fresh, pad_;
 };
 
-struct QMerge {
-  int32_t req, kvh, rt0, B, part0, nparts, pad_[2];
+// what one workgroup takes on: the row tiles from rt0 of one KV head of a piece
+struct QItem : QPiece {
+  int kvh, rt0;
 };
 
 constexpr int kQTile = 64;   // virtual keys per planning unit
 constexpr int kQRowTiles = 4;   // most 32-row tiles (waves) per workgroup
 
 struct QAttnArgs {
-  const QItem* items;
-  const QItem* rows;         // [n]: the requests, whole
-  const QMerge* merges;
-  int n, n_items, n_merge;
+  const QPiece* far;         // the pieces in device memory, or NULL: in `near`
+  QPiece near[kNear];
+  int n_pieces, n_split;
+  int groups;                // workgroups that share a head's row tiles
   int RTW;                   // row tiles per workgroup
   int KS;                    // RTW = 1: waves that share a row's keys (8, 4 or 2)
   int L, Hq, Hkv, D, G, W, S, lt;
@@ -105,7 +131,9 @@ struct QAttnArgs {
   int write_back;
   uint16_t* out;             // [n][L][Hq][D]
   float* parts;              // part_wave_floats(D) per wave of a partial slot
+  __device__ QPiece piece(int i) const { return list_entry(far, near, i); }
 };
+static_assert(sizeof(QAttnArgs) <= 4096, "kernel arguments");
 hipError_t launch_qattn(const QAttnArgs& a, bs_qformat fmt, hipStream_t s);
 
 // ---------------------------------------------------------------- codes

@@ -50,6 +50,14 @@ struct Slot {
   bool held = false;           // a captured graph reads it: never given to another blob
 };
 
+// Host copy of a call's lists that are small enough to travel in the kernel's
+// arguments (the plan is made once per set of descriptors, as for a slot)
+struct NearPlan {
+  std::vector<unsigned char> key, bytes;
+  uint64_t hash = 0, used = 0;
+  int meta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+};
+
 thread_local std::string g_err;
 
 // Hash of a slot's key (keys with equal hashes are compared), eight bytes at a time
@@ -101,6 +109,7 @@ struct bs_ctx {
   int device = 0;
   StaticPath stat;
   std::vector<std::unique_ptr<Slot>> slots;   // stable addresses: calls hold Slot*
+  std::vector<NearPlan> near;
   uint64_t tick = 0;
   std::string err;
   Prof prof;
@@ -306,24 +315,62 @@ int finish(bs_ctx* c, Slot* sl, hipStream_t s, hipError_t launch, const char* wh
   return BS_OK;
 }
 
-// upload() and finish() for calls that may be recorded into a graph. Under
+// upload() and finish() for calls that may be recorded into a graph. Lists of up to
+// `near` bytes stay on the host and go into the launch's arguments: no slot, and no event
+// after the launch (an event takes 2.7 us of host time). Otherwise, under
 // capture nothing may be uploaded and no event of a slot may be recorded (it
 // would become the graph's), so the blob has to be in a slot already: an earlier
 // call put it there. Its upload is waited for here, and the slot then stays as it
 // is until the context goes, since the graph can be replayed until then.
 struct Call {
   Slot* slot = nullptr;
+  const NearPlan* near = nullptr;
   bool captured = false;
+  const int* meta() const { return near ? near->meta : slot->meta; }
+  // lists in device memory: NULL when they are near
+  template <class T>
+  const T* far() const { return near ? nullptr : static_cast<const T*>(slot->d); }
+  template <class T>
+  void fill(T* to) const {
+    if (near) std::memcpy(to, near->bytes.data(), near->bytes.size());
+  }
 };
 
+constexpr size_t kNearPlans = 64;   // sets of descriptors whose plans are kept
+
 template <class Make>
-int begin(bs_ctx* c, hipStream_t s, const Key& key, Make make, Call* call) {
+int begin(bs_ctx* c, hipStream_t s, const Key& key, size_t near, Make make, Call* call) {
+  const uint64_t hv = key_hash(key.b.data(), key.b.size());
+  NearPlan* old = nullptr;
+  for (NearPlan& p : c->near) {
+    if (p.hash == hv && p.key == key.b) {
+      p.used = ++c->tick;
+      call->near = &p;
+      return BS_OK;
+    }
+    if (!old || p.used < old->used) old = &p;
+  }
+  auto live = [&](const std::unique_ptr<Slot>& p) { return p->live && p->hash == hv && p->key == key.b; };
+  Blob blob;
+  if (near && std::none_of(c->slots.begin(), c->slots.end(), live)) {
+    make(blob);
+    if (blob.bytes.size() <= near) {
+      if (c->near.size() < kNearPlans) old = &c->near.emplace_back();
+      old->key = key.b;
+      old->bytes = std::move(blob.bytes);
+      old->hash = hv;
+      old->used = ++c->tick;
+      std::memcpy(old->meta, blob.meta, sizeof old->meta);
+      call->near = old;
+      return BS_OK;
+    }
+  }
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
   hipError_t e = hipStreamIsCapturing(s, &cap);
   if (e != hipSuccess) return hip_fail(c, e, "hipStreamIsCapturing");
-  if (cap == hipStreamCaptureStatusNone) return upload(c, s, key, make, &call->slot);
+  if (cap == hipStreamCaptureStatusNone)
+    return upload(c, s, key, [&](Blob& b) { blob.bytes.empty() ? make(b) : std::swap(b, blob); }, &call->slot);
   call->captured = true;
-  const uint64_t hv = key_hash(key.b.data(), key.b.size());
   for (auto& p : c->slots) {
     Slot& sl = *p;
     if (!sl.live || sl.hash != hv || sl.key != key.b) continue;
@@ -342,7 +389,7 @@ int begin(bs_ctx* c, hipStream_t s, const Key& key, Make make, Call* call) {
 }
 
 int end(bs_ctx* c, const Call& call, hipStream_t s, hipError_t launch, const char* what) {
-  if (!call.captured) return finish(c, call.slot, s, launch, what);
+  if (call.slot && !call.captured) return finish(c, call.slot, s, launch, what);
   return launch == hipSuccess ? BS_OK : hip_fail(c, launch, what);
 }
 
@@ -933,8 +980,8 @@ struct QRows {
   int tiles, groups, per;   // row tiles of a head, workgroups, row tiles per workgroup
 };
 
-// requests times KV heads of one call: bounds the work list (at most four workgroups
-// for each and a round of pieces, 40 bytes) and every index made from it
+// requests times KV heads of one call: bounds every index made from the list of pieces
+// (the rows and at most a round of workgroups more)
 constexpr int kMaxQRows = 1 << 20;
 
 QRows qattn_rows(int L, int Hq, int Hkv) {
@@ -945,19 +992,20 @@ QRows qattn_rows(int L, int Hq, int Hkv) {
   return q;
 }
 
-QItem qattn_row(const bs_req_desc& r, int i, int L) {
+QPiece qattn_row(const bs_req_desc& r, int i, int L) {
   const Geo geo = geo_of(r, L);
-  QItem it{};
+  QPiece it{};
   it.req = i; it.row = r.row; it.off = r.off; it.s = geo.s; it.B = (uint8_t)geo.B;   // L <= 64
   it.pad = (uint8_t)group_pad(r.p, 6);
   it.nv = geo.len > geo.B ? it.pad + geo.len - geo.B : 0;
   it.v1 = it.nv;
   it.part = -1;
+  it.np = 1;
   it.fresh = 1;
   return it;
 }
 
-int qattn_tiles(const QItem& it) { return std::max(1, (it.nv + kQTile - 1) / kQTile); }
+int qattn_tiles(const QPiece& it) { return std::max(1, (it.nv + kQTile - 1) / kQTile); }
 
 // How a launch cuts its rows: rows of more than `cap` 64-key tiles into even pieces
 // of at most that (0: none); `ks`: waves that share a row's keys, for heads of one
@@ -1042,59 +1090,40 @@ size_t qattn_part_bytes(int parts, const QRows& q, int D) {
   return (size_t)parts * q.per * part_wave_floats(D) * sizeof(float);
 }
 
-// meta = {items, item count, merges, merge count, partial slots, whole rows, QPlan::ks}
+// meta = {pieces, split rows, partial slots, QPlan::ks}
 void qattn_blob(Blob& blob, const bs_req_desc* reqs, int n, int L, int Hq, int Hkv, bool split) {
   const QRows q = qattn_rows(L, Hq, Hkv);
   const QPlan plan = split ? qattn_plan(reqs, n, L, Hkv, q) : QPlan{0, qattn_waves((size_t)n * Hkv)};
   const int cap = plan.cap;
-  // a request's pieces are alike for all its heads: cut and sort one head's
-  std::vector<QItem> pieces, rows((size_t)n);
-  std::vector<QMerge> merges;
+  // a request's pieces are alike for all its heads: the list names one head's
+  std::vector<QPiece> pieces;
   pieces.reserve((size_t)n);
-  int parts = 0;
+  int parts = 0, split_rows = 0;
   for (int i = 0; i < n; ++i) {
-    const QItem row = rows[i] = qattn_row(reqs[i], i, L);
+    const QPiece row = qattn_row(reqs[i], i, L);
     const int nt = qattn_tiles(row), np = cap > 0 && nt > cap ? (nt + cap - 1) / cap : 1;
     for (int k = 0; k < np; ++k) {
-      QItem it = row;
+      QPiece it = row;
+      it.np = np;
       if (np > 1) {
         it.v0 = (int)((int64_t)k * nt / np) * kQTile;          // even pieces
         it.v1 = std::min(row.nv, (int)((int64_t)(k + 1) * nt / np) * kQTile);
-        it.part = parts + k;         // of the first head's first workgroup; the others' follow, np apart
+        it.part = parts + k;         // the other heads' and workgroups' follow, np apart
         it.fresh = k == 0;
       }
       pieces.push_back(it);
     }
-    if (np > 1)
-      for (int h = 0; h < Hkv; ++h)
-        for (int gr = 0; gr < q.groups; ++gr, parts += np) merges.push_back(QMerge{i, h, gr * q.per, row.B, parts, np, {0, 0}});
+    if (np > 1) parts += np * Hkv * q.groups;
   }
-  // longest first; the workgroups of a piece, which read the same keys, stand eight
-  // apart, which is the same XCD and its L2
-  std::stable_sort(pieces.begin(), pieces.end(), [](const QItem& x, const QItem& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
-  std::vector<QItem> items;
-  const size_t heads = pieces.size() * Hkv;
-  items.reserve(heads * q.groups);
-  for (size_t b = 0; b < heads; b += 8)
-    for (int gr = 0; gr < q.groups; ++gr)
-      for (size_t k = b; k < std::min(b + 8, heads); ++k) {
-        QItem it = pieces[k / Hkv];
-        const int h = (int)(k % Hkv);
-        it.kvh = (uint16_t)h;
-        it.rt0 = (uint16_t)(gr * q.per);
-        if (it.part >= 0) {
-          const int nt = qattn_tiles(rows[it.req]), np = (nt + cap - 1) / cap;
-          it.part += (h * q.groups + gr) * np;
-        }
-        items.push_back(it);
-      }
-  blob.meta[0] = (int)blob.add(items.data(), sizeof(QItem) * items.size());
-  blob.meta[1] = (int)items.size();
-  blob.meta[2] = (int)blob.add(merges.data(), sizeof(QMerge) * merges.size());
-  blob.meta[3] = (int)merges.size();
-  blob.meta[4] = parts;
-  blob.meta[5] = (int)blob.add(rows.data(), sizeof(QItem) * rows.size());
-  blob.meta[6] = plan.ks;
+  // longest first
+  std::stable_sort(pieces.begin(), pieces.end(), [](const QPiece& x, const QPiece& y) { return x.v1 - x.v0 > y.v1 - y.v0; });
+  for (size_t i = 0; i < pieces.size(); ++i)
+    if (pieces[i].part >= 0 && pieces[i].fresh) pieces[(size_t)split_rows++].split = (int)i;
+  blob.add(pieces.data(), sizeof(QPiece) * pieces.size());
+  blob.meta[0] = (int)pieces.size();
+  blob.meta[1] = split_rows;
+  blob.meta[2] = parts;
+  blob.meta[3] = plan.ks;
 }
 
 int longest_row(const bs_req_desc* reqs, int n) {
@@ -1573,10 +1602,14 @@ int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int 
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Call call;
-  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
-  if (st) return st;
   QuantArgs a{};
-  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
+  if (n <= kNear) {
+    std::memcpy(a.reqs.near, reqs, sizeof(bs_req_desc) * n);
+  } else {
+    st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), 0, [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
+    if (st) return st;
+    a.reqs.far = call.far<bs_req_desc>();
+  }
   a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.k = k; a.v = v;
   a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
@@ -1605,10 +1638,14 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Call call;
-  st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
-  if (st) return st;
   DequantArgs a{};
-  a.reqs = static_cast<const bs_req_desc*>(call.slot->d);
+  if (n <= kNear) {
+    std::memcpy(a.reqs.near, reqs, sizeof(bs_req_desc) * n);
+  } else {
+    st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), 0, [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
+    if (st) return st;
+    a.reqs.far = call.far<bs_req_desc>();
+  }
   a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.k8 = static_cast<const uint8_t*>(k8); a.v8 = static_cast<const uint8_t*>(v8);
   a.k_scale = k_scale; a.v_scale = v_scale;
@@ -1664,23 +1701,22 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   const QRows q_rows = qattn_rows(L, Hq, Hkv);
   Call call;
   for (int split = ws ? 1 : 0; split >= 0; --split) {
-    st = begin(c, s, Key('K', {n, L, Hq, Hkv, split}, reqs, sizeof(bs_req_desc) * n),
+    call = Call{};
+    st = begin(c, s, Key('K', {n, L, Hq, Hkv, split}, reqs, sizeof(bs_req_desc) * n), sizeof(QPiece) * kNear,
                [&](Blob& blob) { qattn_blob(blob, reqs, n, L, Hq, Hkv, split != 0); }, &call);
     if (st) return st;
-    if (qattn_part_bytes(call.slot->meta[4], q_rows, D) <= ws_bytes) break;
+    if (qattn_part_bytes(call.meta()[2], q_rows, D) <= ws_bytes) break;
   }
-  const char* base = static_cast<const char*>(call.slot->d);
-  const int* meta = call.slot->meta;
+  const int* meta = call.meta();
   QAttnArgs a{};
-  a.items = reinterpret_cast<const QItem*>(base + meta[0]);
-  a.n_items = meta[1];
-  a.merges = reinterpret_cast<const QMerge*>(base + meta[2]);
-  a.n_merge = meta[3];
-  a.rows = reinterpret_cast<const QItem*>(base + meta[5]);
-  a.n = n;
+  a.far = call.far<QPiece>();
+  call.fill(a.near);
+  a.n_pieces = meta[0];
+  a.n_split = meta[1];
   a.parts = static_cast<float*>(ws);
+  a.groups = q_rows.groups;
   a.RTW = q_rows.per;
-  a.KS = meta[6];
+  a.KS = meta[3];
   a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.scale_log2e = (scale > 0.0f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   a.q = static_cast<const uint16_t*>(q);
@@ -1736,7 +1772,7 @@ int bs_qk_norm_rope(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int
   uint32_t base_bits;
   std::memcpy(&base_bits, &rope_base, sizeof base_bits);
   Call call;
-  st = begin(c, s, Key('N', {n, rope ? D : 0, rope ? (int64_t)base_bits : 0}, reqs, sizeof(bs_req_desc) * n),
+  st = begin(c, s, Key('N', {n, rope ? D : 0, rope ? (int64_t)base_bits : 0}, reqs, sizeof(bs_req_desc) * n), 0,
              [&](Blob& b) {
                b.meta[0] = (int)b.add(reqs, sizeof(bs_req_desc) * n);
                std::vector<float2> freq(rope ? (size_t)D / 2 : 0);

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
   constexpr int GS = D / F;           // lanes per token
   constexpr int RS = 64 / GS;         // tokens per step
   constexpr int CT = RS * RP;         // tokens per wave
-  const bs_req_desc r = a.reqs[blockIdx.y];
+  const bs_req_desc r = a.reqs.get(blockIdx.y);
   const int h = blockIdx.z >> 1, tensor = blockIdx.z & 1;
   const int lane = threadIdx.x & 63, T = 1 << a.lt;
   const int pad = group_pad(r.p, a.lt), len = r.p + r.g;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a) {
 template <typename E, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_dequantize(DequantArgs a) {
   constexpr int F = 16 / sizeof(E), GS = D / F;       // features per lane, lanes per token
-  const bs_req_desc r = a.reqs[blockIdx.y];
+  const bs_req_desc r = a.reqs.get(blockIdx.y);
   const int h = blockIdx.z >> 1, tensor = blockIdx.z & 1;
   const int u = blockIdx.x * 256 + threadIdx.x;
   const int t = u / GS;

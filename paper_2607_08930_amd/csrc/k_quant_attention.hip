@@ -105,7 +105,7 @@ __device__ inline int swz16(int row) {
 // row tiles the same way: a CU holds one such workgroup, so these would run after
 // the others, 3 us.)
 template <int FMT, int D, int RP, class Row>
-__device__ inline void store_block(const QAttnArgs& a, const QItem& it, int c, int tensor, int lane, Row row) {
+__device__ inline void store_block(const QAttnArgs& a, const QPiece& it, int c, int tensor, int lane, Row row) {
   constexpr int GS = D / 16, RS = 64 / GS;
   const int col = (lane % GS) * 16, T = 1 << a.lt;
   float top[RP];
@@ -139,14 +139,37 @@ __device__ inline void store_block(const QAttnArgs& a, const QItem& it, int c, i
   }
 }
 
-// Unit u of the launch's last workgroups: one tensor of one (request, KV head)
+// a quotient of uniform numbers, which comes out of the vector unit, back in a scalar register
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// What workgroup b takes on. The pieces' heads are counted piece by piece; the workgroups
+// of a head, which read the same keys, stand eight apart, which is the same XCD and
+// its L2.
+__device__ inline QItem item_of(const QAttnArgs& a, int b) {
+  int k = b, gr = 0;
+  if (a.groups > 1) {
+    const int k0 = uniform(b / (8 * a.groups)) * 8, left = a.n_pieces * a.Hkv - k0, w = left < 8 ? left : 8, u = b - k0 * a.groups;
+    gr = uniform(u / w);
+    k = k0 + u - gr * w;
+  }
+  const int i = uniform(k / a.Hkv);
+  QItem it;
+  static_cast<QPiece&>(it) = a.piece(i);
+  it.kvh = k - i * a.Hkv;
+  it.rt0 = gr * a.RTW;
+  if (it.part >= 0) it.part += (it.kvh * a.groups + gr) * it.np;
+  return it;
+}
+
+// Unit u of the launch's last workgroups: one tensor of one (piece, KV head)
 template <int FMT, int D>
 __device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
   constexpr int GS = D / 16, RS = 64 / GS, RP = 32 / RS;   // a single row tile: L <= 32
-  if (u >= a.n * a.Hkv * 2) return;
-  const int tensor = u & 1, c = (u >> 1) % a.Hkv, i = (u >> 1) / a.Hkv;
-  const QItem it = a.rows[i];
-  const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)i * a.L * a.Hkv + c) * D + (lane % GS) * 16;
+  if (u >= a.n_pieces * a.Hkv * 2) return;
+  const int tensor = u & 1, i = uniform((u >> 1) / a.Hkv), c = (u >> 1) - i * a.Hkv;
+  const QPiece it = a.piece(i);
+  if (!it.fresh) return;
+  const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)it.req * a.L * a.Hkv + c) * D + (lane % GS) * 16;
   v4u x[RP][2];
 #pragma unroll
   for (int p = 0; p < RP; ++p) {
@@ -319,11 +342,12 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
   __shared__ __align__(1024) uint8_t rings[KS * RING];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x >= a.n_items) {
-    quantize_block<FMT, D>(a, ((int)blockIdx.x - a.n_items) * KS + w, threadIdx.x & 63);
+  const int items = a.n_pieces * a.Hkv;
+  if ((int)blockIdx.x >= items) {
+    quantize_block<FMT, D>(a, ((int)blockIdx.x - items) * KS + w, threadIdx.x & 63);
     return;
   }
-  const QItem it = a.items[blockIdx.x];
+  const QItem it = item_of(a, blockIdx.x);
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31, q16 = lane >> 4, j16 = lane & 15;
   const Keys<D> kk_(a, it);
   const int pad = kk_.pad, nv = kk_.nv, r = it.rt0 * 32 + n;
@@ -643,7 +667,7 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
   __shared__ __align__(1024) uint8_t ring[NS * STAGE + NS * SCB];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const QItem it = a.items[blockIdx.x];
+  const QItem it = item_of(a, blockIdx.x);
   const int lane = threadIdx.x & 63, g = lane >> 5, n = lane & 31, q16 = lane >> 4, j16 = lane & 15;
   const Keys<D> keys(a, it);
   const int B = it.B, pad = it.pad, nv = it.nv, v0 = it.v0, v1 = it.v1;
@@ -1046,19 +1070,21 @@ template <int D>
 __global__ __launch_bounds__(256) void k_qattn_merge(QAttnArgs a) {
   constexpr int NG = D / 8, CH = kMergeBatch;
   const int wv = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  if (wv >= a.n_merge * a.RTW * NG) return;
-  const int k = wv % NG, t = wv / NG % a.RTW;
-  const QMerge mg = a.merges[wv / NG / a.RTW];
+  const int heads = a.Hkv * a.groups;
+  if (wv >= a.n_split * heads * a.RTW * NG) return;
+  const int k = wv % NG, tw = uniform(wv / NG / a.RTW), t = wv / NG - tw * a.RTW;
+  const int mi = uniform(tw / heads), hg = tw - mi * heads;
+  const QPiece mg = a.piece(a.piece(mi).split);
   const int64_t stride = (int64_t)a.RTW * part_wave_floats(D);
-  const float* pw = a.parts + ((int64_t)mg.part0 * a.RTW + t) * part_wave_floats(D);
+  const float* pw = a.parts + ((int64_t)(mg.part + hg * mg.np) * a.RTW + t) * part_wave_floats(D);
   f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
   float m = -__builtin_inff(), l = 0.0f;
-  for (int p0 = 0; p0 < mg.nparts; p0 += CH) {
+  for (int p0 = 0; p0 < mg.np; p0 += CH) {
     float mp[CH], lp[CH];
     f32x4_t op[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const bool ok = p0 + i < mg.nparts;
+      const bool ok = p0 + i < mg.np;
       const float* pp = pw + (ok ? p0 + i : p0) * stride;
       mp[i] = ok ? pp[NG * 256 + lane] : -__builtin_inff();
       lp[i] = pp[NG * 256 + 64 + lane];
@@ -1078,12 +1104,12 @@ __global__ __launch_bounds__(256) void k_qattn_merge(QAttnArgs a) {
     }
     m = mn;
   }
-  const int r = (mg.rt0 + t) * 32 + (lane & 31);
+  const int kvh = uniform(hg / a.groups), r = ((hg - kvh * a.groups) * a.RTW + t) * 32 + (lane & 31);
   if (r >= a.G * a.L) return;
   const float inv = 1.0f / l;
   typedef uint32_t v2u __attribute__((ext_vector_type(2)));
   const v2u y = {pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
-  *reinterpret_cast<v2u*>(out_row<D>(a, mg.req, mg.kvh, r, 1.0f / (float)a.G) + 8 * k + 4 * (lane >> 5)) =
+  *reinterpret_cast<v2u*>(out_row<D>(a, mg.req, kvh, r, 1.0f / (float)a.G) + 8 * k + 4 * (lane >> 5)) =
       r < a.G * mg.B ? y : v2u{0, 0};
 }
 
@@ -1091,8 +1117,8 @@ template <int FMT, int D>
 void attend(const QAttnArgs& a, hipStream_t s) {
   auto go = [&](auto kernel, int waves) {
     // one row tile: workgroups that write the blocks into the cache stand last
-    const int wb = a.write_back && a.RTW == 1 ? (a.n * a.Hkv * 2 + waves - 1) / waves : 0;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.n_items + wb)), dim3((unsigned)(64 * waves)), 0, s, a);
+    const int heads = a.n_pieces * a.Hkv, wb = a.write_back && a.RTW == 1 ? (heads * 2 + waves - 1) / waves : 0;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(heads * a.groups + wb)), dim3((unsigned)(64 * waves)), 0, s, a);
   };
   auto by_groups = [&](auto uni_tag) {
     constexpr bool UNI = decltype(uni_tag)::value != 0;
@@ -1106,8 +1132,9 @@ void attend(const QAttnArgs& a, hipStream_t s) {
       go(k_qattn_keys<FMT, D, 2, UNI>, 2);
   };
   a.lt >= 5 ? by_groups(QInt<1>{}) : by_groups(QInt<0>{});
-  if (a.n_merge)
-    hipLaunchKernelGGL(k_qattn_merge<D>, dim3((unsigned)((a.n_merge * a.RTW * (D / 8) + 3) / 4)), dim3(256), 0, s, a);
+  if (a.n_split)
+    hipLaunchKernelGGL(k_qattn_merge<D>, dim3((unsigned)(((int64_t)a.n_split * a.Hkv * a.groups * a.RTW * (D / 8) + 3) / 4)), dim3(256), 0,
+                       s, a);
 }
 
 }  // namespace

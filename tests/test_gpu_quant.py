@@ -427,14 +427,19 @@ def test_captured_and_replayed(ctx):
         bs.bs_kv_dequantize(ctx, w["reqs"], 32, w["R"], w["W"], 4, 128, bs.BS_BF16, 0, 32, d["k8"], d["v8"], d["k_scale"],
                             d["v_scale"], w["S"], box, box2)
 
-    # descriptors that no call outside a capture has uploaded are refused
+    # lists that a launch cannot carry, and that no call outside a capture has uploaded, are refused
     fresh = bs.Context(0)
-    g = torch.cuda.CUDAGraph()
-    with pytest.raises(bs.BlockServeError, match="captured"):
-        with torch.cuda.graph(g):
-            torch.zeros(1, device="cuda").add_(1)
-            bs.bs_kv_dequantize(fresh, w["reqs"], 32, w["R"], w["W"], 4, 128, bs.BS_BF16, 0, 32, d["k8"], d["v8"],
-                                d["k_scale"], d["v_scale"], w["S"], box, box2)
+    many = np.zeros(80, bs.REQ_DTYPE)
+    many["p"], many["g"], many["row"] = 1, 2, np.arange(80)
+    small = [torch.zeros(80 * 4 * 3 * 128, dtype=torch.bfloat16, device="cuda") for _ in range(6)]
+    for call in (lambda: bs.bs_kv_dequantize(fresh, many, 2, 80, 3, 4, 128, bs.BS_BF16, 0, 2, *small[:2], *small[2:4], 3, *small[4:]),
+                 lambda: bs.bs_qk_norm_rope(fresh, w["reqs"], 32, w["R"], w["W"], False, 4, 4, 128, bs.BS_BF16, d["q"], 512, d["k_new"],
+                                            512, None, None, 1e-6, 1e4, qo, ko)):
+        g = torch.cuda.CUDAGraph()
+        with pytest.raises(bs.BlockServeError, match="captured"):
+            with torch.cuda.graph(g):
+                torch.zeros(1, device="cuda").add_(1)
+                call()
     fresh.close()
     calls()
     torch.cuda.synchronize()
@@ -455,6 +460,67 @@ def test_captured_and_replayed(ctx):
         torch.cuda.synchronize()
         for x, y in zip((d["out"], box, box2, d["k8"], d["k_scale"]), want):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), f"replay {rep}"
+
+
+def test_captured_by_a_context_that_never_ran():
+    # short lists travel with the launch: nothing has to be there before
+    torch, bs, _ = lazy()
+    rng = np.random.default_rng(17)
+    w = attention_case(rng, [(300, 64, 1), (2100, 64, 0)], 32, 14, 2, 128, 32, "e4m3")
+    d = on_device(w)
+    need = bs.bs_quant_attention_workspace_bytes(w["reqs"], 32, 14, 2, 128)
+    assert need > 0                                # the long row is split: two launches
+    ws = torch.full((need,), 0xA5, dtype=torch.uint8, device="cuda")
+    box = [torch.zeros((w["R"], 2, w["W"], 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    with bs.Context(0) as ctx:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            attend(ctx, w, d, ws=ws)
+            bs.bs_kv_dequantize(ctx, w["reqs"], 32, w["R"], w["W"], 2, 128, bs.BS_BF16, 0, 32, d["k8"], d["v8"], d["k_scale"],
+                                d["v_scale"], w["S"], *box)
+        for _ in range(3):
+            d["out"].fill_(float("nan"))
+            for x in box:
+                x.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            check_out(w, d)
+            check_cache(w, d, True)
+            for i, r in enumerate(w["reqs"]):
+                t = oracle.geometry(r, 32)
+                for c in range(2):
+                    num = quant.row_numbers(r, c, d["v8"].cpu().numpy(), d["v_scale"].cpu().numpy(), 32, "e4m3")
+                    got = box[1][t.row, c, t.off:t.off + len(num)].float().cpu().numpy()
+                    assert (np.abs(got - num) <= 2.0 ** -8 * np.abs(num)).all()
+
+
+@pytest.mark.parametrize("n", [64, 65, 130])
+def test_lists_that_travel_with_the_launch_and_longer_ones(ctx, n):
+    torch, bs, bstep = lazy()
+    rng = np.random.default_rng(n)
+    lens = [(int(rng.integers(0, 70)), int(rng.integers(1, 40)), 0) for _ in range(n - 1)] + [(1500, 40, 0)]
+    w = attention_case(rng, lens, 8, 10, 2, 64, 8, "i8")
+    d = on_device(w)
+    attend(ctx, w, d)
+    torch.cuda.synchronize()
+    say(f"n={n}: {check_out(w, d):.3f} of the bound")
+    check_cache(w, d, True)
+    for dt, tol in (("bf16", 2.0 ** -8), ("f32", 2.0 ** -24)):
+        box = [torch.zeros((w["R"], 2, w["W"], 64), dtype=bstep.torch_dtype(dt), device="cuda") for _ in range(2)]
+        again = [torch.zeros_like(d["k8"]) for _ in range(2)] + [torch.zeros_like(d["k_scale"]) for _ in range(2)]
+        bs.bs_kv_dequantize(ctx, w["reqs"], 8, w["R"], w["W"], 2, 64, bstep.dt_code(dt), 1, 8, d["k8"], d["v8"], d["k_scale"],
+                            d["v_scale"], w["S"], *box)
+        bs.bs_kv_quantize(ctx, w["reqs"], 8, w["R"], w["W"], 2, 64, bstep.dt_code(dt), 1, 8, *box, *again, w["S"])
+        torch.cuda.synchronize()
+        codes, scales = d["k8"].cpu().numpy(), d["k_scale"].cpu().numpy()
+        rc, rs = quant.kv_quantize(w["reqs"], bstep.to_host(box[0]), np.zeros_like(codes), np.zeros_like(scales), 8, "i8", dt)
+        np.testing.assert_array_equal(again[0].cpu().numpy(), rc)
+        np.testing.assert_array_equal(again[2].cpu().numpy(), rs)
+        for r in w["reqs"]:
+            for c in range(2):
+                num = quant.row_numbers(r, c, codes, scales, 8, "i8")
+                got = box[0][r["row"], c, r["off"]:r["off"] + len(num)].double().cpu().numpy()
+                assert (np.abs(got - num) <= tol * np.abs(num)).all()
 
 
 def test_refusals(ctx):
