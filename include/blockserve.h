@@ -351,9 +351,10 @@ int bs_dual_cache_refresh(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, in
  * with D = 4 and W = S / 4, segments of ceil(groups / 4) cells from column 0.
  *
  * Under stream capture the calls below that take a context can be
- * recorded into a graph: the same descriptors (with the same shape arguments)
- * must have gone through the same call on that context outside a capture
- * before, which uploads them; otherwise BS_ERR_UNSUPPORTED. The upload then
+ * recorded into a graph. Lists of up to 64 requests (for the attention: of pieces,
+ * where it splits rows) travel in the launch's arguments. Longer ones must have gone
+ * through the same call with the same shape arguments on that context outside a
+ * capture before, which uploads them; otherwise BS_ERR_UNSUPPORTED. The upload then
  * stays in its slot until the context is destroyed, and graphs that hold the
  * call must not be replayed after that. Graphs whose replays may overlap need
  * workspaces of their own, like calls that may overlap.
@@ -441,7 +442,10 @@ int bs_quant_cache_block_attention(bs_ctx* ctx, const bs_req_desc* reqs, int n, 
  * q_weight, k_weight: [D] of dt, or NULL for ones. eps < 0 leaves the norm out
  * (the weights are not read), rope_base <= 0 the rotation.
  * Supported: dt BS_BF16 or BS_F32, D a multiple of 16 up to 256, W < 2^24,
- * n <= 65535; pointers 16-byte aligned, strides a multiple of 16 bytes.
+ * n <= 65535; pointers 16-byte aligned, strides a multiple of 16 bytes. The first
+ * call with a pair of rope_base and D makes a table and waits for its upload; it is
+ * refused under capture, as is the 65th pair of a context (BS_ERR_UNSUPPORTED). Graphs
+ * must not be replayed after their context is destroyed.
  */
 int bs_qk_norm_rope(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, int W, int whole_rows, int Hq, int Hkv,
                     int D, bs_dtype dt, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

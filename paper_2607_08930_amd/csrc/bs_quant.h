@@ -45,7 +45,7 @@ struct ReqList {
 };
 
 struct NormRopeArgs {
-  const bs_req_desc* reqs;
+  ReqList reqs;
   const float2* freq;        // [D / 2]: turns per position of feature pair f, as high + low part
   int L, W, Hq, Hkv, D;
   int rows;                  // 0: blocks [n][L], 1: whole rows of the box [R][W]

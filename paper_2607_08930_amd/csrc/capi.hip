@@ -58,6 +58,13 @@ struct NearPlan {
   int meta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 };
 
+struct RopeTable {
+  int D;
+  float base;
+  float2* d;
+};
+constexpr size_t kRopeTables = 64;
+
 thread_local std::string g_err;
 
 // Hash of a slot's key (keys with equal hashes are compared), eight bytes at a time
@@ -110,6 +117,7 @@ struct bs_ctx {
   StaticPath stat;
   std::vector<std::unique_ptr<Slot>> slots;   // stable addresses: calls hold Slot*
   std::vector<NearPlan> near;
+  std::vector<RopeTable> rope;
   uint64_t tick = 0;
   std::string err;
   Prof prof;
@@ -391,6 +399,53 @@ int begin(bs_ctx* c, hipStream_t s, const Key& key, size_t near, Make make, Call
 int end(bs_ctx* c, const Call& call, hipStream_t s, hipError_t launch, const char* what) {
   if (call.slot && !call.captured) return finish(c, call.slot, s, launch, what);
   return launch == hipSuccess ? BS_OK : hip_fail(c, launch, what);
+}
+
+// a list of requests alone
+int begin_reqs(bs_ctx* c, hipStream_t s, const bs_req_desc* reqs, int n, ReqList* to, Call* call) {
+  if (n <= kNear) {
+    std::memcpy(to->near, reqs, sizeof(bs_req_desc) * n);
+    return BS_OK;
+  }
+  const int st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), 0, [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, call);
+  if (!st) to->far = call->far<bs_req_desc>();
+  return st;
+}
+
+// The turns per position of each feature pair, high and low part, for heads of D
+// features: made and uploaded by the first call that needs them, then kept
+int rope_table(bs_ctx* c, hipStream_t s, int D, float base, const float2** out) {
+  for (const RopeTable& t : c->rope)
+    if (t.D == D && t.base == base) {
+      *out = t.d;
+      return BS_OK;
+    }
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(s, &cap);
+  if (e != hipSuccess) return hip_fail(c, e, "hipStreamIsCapturing");
+  if (cap != hipStreamCaptureStatusNone)
+    return fail(c, BS_ERR_UNSUPPORTED, "the stream is being captured: rotate once with this base and D outside a capture first");
+  if (c->rope.size() >= kRopeTables)
+    return fail(c, BS_ERR_UNSUPPORTED, "the context keeps %d pairs of rope_base and D", (int)kRopeTables);
+  std::vector<float2> freq((size_t)D / 2);
+  for (size_t f = 0; f < freq.size(); ++f) {
+    const double turns = std::exp2(-2.0 * (double)f / D * std::log2((double)base)) / 6.283185307179586476925;
+    freq[f].x = (float)turns;
+    freq[f].y = (float)(turns - (double)freq[f].x);
+  }
+  c->rope.reserve(kRopeTables);
+  void* d = nullptr;
+  e = hipMalloc(&d, sizeof(float2) * freq.size());
+  if (e != hipSuccess) return hip_fail(c, e, "hipMalloc(rotation)");
+  e = hipMemcpyAsync(d, freq.data(), sizeof(float2) * freq.size(), hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipStreamSynchronize(s);      // every stream may read it from here on
+  if (e != hipSuccess) {
+    (void)hipFree(d);
+    return hip_fail(c, e, "upload of the rotation");
+  }
+  c->rope.push_back(RopeTable{D, base, static_cast<float2*>(d)});
+  *out = c->rope.back().d;
+  return BS_OK;
 }
 
 int dtype_bytes(bs_dtype dt) { return dt == BS_F32 ? 4 : (dt == BS_BF16 ? 2 : 0); }
@@ -1211,6 +1266,7 @@ int bs_destroy(bs_ctx* c) {
     if (sl.ready) (void)hipEventDestroy(sl.ready);
     if (sl.done) (void)hipEventDestroy(sl.done);
   }
+  for (const RopeTable& t : c->rope) (void)hipFree(t.d);
   delete c;
   return BS_OK;
 }
@@ -1603,13 +1659,8 @@ int bs_kv_quantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int 
   hipStream_t s = static_cast<hipStream_t>(stream);
   Call call;
   QuantArgs a{};
-  if (n <= kNear) {
-    std::memcpy(a.reqs.near, reqs, sizeof(bs_req_desc) * n);
-  } else {
-    st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), 0, [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
-    if (st) return st;
-    a.reqs.far = call.far<bs_req_desc>();
-  }
+  st = begin_reqs(c, s, reqs, n, &a.reqs, &call);
+  if (st) return st;
   a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.k = k; a.v = v;
   a.k8 = static_cast<uint8_t*>(k8); a.v8 = static_cast<uint8_t*>(v8);
@@ -1639,13 +1690,8 @@ int bs_kv_dequantize(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, in
   hipStream_t s = static_cast<hipStream_t>(stream);
   Call call;
   DequantArgs a{};
-  if (n <= kNear) {
-    std::memcpy(a.reqs.near, reqs, sizeof(bs_req_desc) * n);
-  } else {
-    st = begin(c, s, Key('Q', {n}, reqs, sizeof(bs_req_desc) * n), 0, [&](Blob& b) { b.add(reqs, sizeof(bs_req_desc) * n); }, &call);
-    if (st) return st;
-    a.reqs.far = call.far<bs_req_desc>();
-  }
+  st = begin_reqs(c, s, reqs, n, &a.reqs, &call);
+  if (st) return st;
   a.Hkv = Hkv; a.W = W; a.S = S; a.lt = group_shift(T);
   a.k8 = static_cast<const uint8_t*>(k8); a.v8 = static_cast<const uint8_t*>(v8);
   a.k_scale = k_scale; a.v_scale = v_scale;
@@ -1769,26 +1815,14 @@ int bs_qk_norm_rope(bs_ctx* c, const bs_req_desc* reqs, int n, int L, int R, int
   if (!dg.ok) return fail(c, BS_ERR_HIP, "hipSetDevice(%d) failed", c->device);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool rope = rope_base > 0.0f;
-  uint32_t base_bits;
-  std::memcpy(&base_bits, &rope_base, sizeof base_bits);
-  Call call;
-  st = begin(c, s, Key('N', {n, rope ? D : 0, rope ? (int64_t)base_bits : 0}, reqs, sizeof(bs_req_desc) * n), 0,
-             [&](Blob& b) {
-               b.meta[0] = (int)b.add(reqs, sizeof(bs_req_desc) * n);
-               std::vector<float2> freq(rope ? (size_t)D / 2 : 0);
-               for (size_t f = 0; f < freq.size(); ++f) {
-                 const double turns = std::exp2(-2.0 * (double)f / D * std::log2((double)rope_base)) / 6.283185307179586476925;
-                 freq[f].x = (float)turns;
-                 freq[f].y = (float)(turns - (double)freq[f].x);
-               }
-               b.meta[1] = (int)b.add(freq.data(), sizeof(float2) * freq.size());
-             },
-             &call);
-  if (st) return st;
-  const char* base = static_cast<const char*>(call.slot->d);
   NormRopeArgs a{};
-  a.reqs = reinterpret_cast<const bs_req_desc*>(base + call.slot->meta[0]);
-  a.freq = reinterpret_cast<const float2*>(base + call.slot->meta[1]);
+  if (rope) {
+    st = rope_table(c, s, D, rope_base, &a.freq);
+    if (st) return st;
+  }
+  Call call;
+  st = begin_reqs(c, s, reqs, n, &a.reqs, &call);
+  if (st) return st;
   a.L = L; a.W = W; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
   a.rows = whole_rows ? 1 : 0;
   a.norm = eps >= 0.0f ? 1 : 0;

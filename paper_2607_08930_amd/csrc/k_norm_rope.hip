@@ -55,7 +55,7 @@ __device__ inline void store8(E* p, const float (&y)[8]) {
 // GS lanes per head row, of which D / 16 work (GS = D / 16 rounded up to a power of 2)
 template <typename E, int GS>
 __global__ __launch_bounds__(256) void k_norm_rope(NormRopeArgs a) {
-  const bs_req_desc r = a.reqs[blockIdx.y];
+  const bs_req_desc r = a.reqs.get(blockIdx.y);
   const Geo geo = geo_of(r, a.L);
   const int D = a.D, H = a.Hq + a.Hkv, NHC = (H + kHeads - 1) / kHeads;
   const int u = (blockIdx.x * 256 + threadIdx.x) / GS, c = threadIdx.x % GS;
