@@ -224,11 +224,11 @@ struct Column {
       t = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{pp[i >> 2][2 * (i & 3)], pp[i >> 2][2 * (i & 3) + 1]}, one, t, false);
     return t;
   }
-  // weights 2^(s - m) times the keys' own V scales
-  __device__ void weights_by_key(const f32x16_t& s, const f32x4_t (&vs)[4]) {
+  // weights 2^(s f - m) times the keys' own V scales
+  __device__ void weights_by_key(const f32x16_t& s, float f, const f32x4_t (&vs)[4]) {
 #pragma unroll
     for (int rr = 0; rr < 16; ++rr) {
-      const float y = __builtin_amdgcn_exp2f(s[rr] - mrun);
+      const float y = __builtin_amdgcn_exp2f(fmaf(s[rr], f, -mrun));
       lsum += y;
       pp[rr >> 3][rr & 7] = (__bf16)(y * vs[rr >> 2][rr & 3]);
     }
@@ -319,6 +319,73 @@ struct Keys {
   // a key that exists: those before the first and past the last repeat it (masked later)
   __device__ int clamp(int x) const { return min(max(x, pad), nv - 1); }
   __device__ bool whole(int x, int n) const { return x >= pad && x + n <= nv && (x + n <= seam || x >= seam); }
+};
+
+// ---------------------------------------------------------------- queries in the codes' terms
+// The queries as numbers of the codes' own kind, so that codes enter the scores' MFMAs
+// as they are: a query is the sum of two of them, which costs two MFMAs of twice the
+// bf16 rate (no more time) and saves the widening of K (32 to 96 VALU instructions a
+// sub-tile).
+//   e4m3: x 2^k = hi + lo, k putting the row's largest element into [128, 256). hi
+//         holds the four leading bits, lo the four that are left of a bf16 number; lo
+//         loses at most 2^-10, which is 2^-17 of the row's largest.
+//   int8: x 16256 / max|x| rounded to an integer (2^-15 of the largest) = 128 hi + lo;
+//         the sums of hi are shifted by 7 before lo's are added. |128 hi + lo| <=
+//         16256, so the sums stay below 128 * 16256 * 128 < 2^29.
+// Lane (g, n) of operand i holds features 32 i + 16 g .. + 15, as a 16-byte read of K
+// finds them; e4m3's MFMAs take operands 2 j and 2 j + 1 together.
+template <int FMT, int D>
+struct SplitQueries {
+  static constexpr int N = D / 32;
+  i32x4_t hi[N], lo[N];
+  float back;              // a score in these units times this is the score
+
+  __device__ void set(const bf16x8_t (&qb)[D / 16]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qb[i][e]));
+    top = max_across<32>(top);             // the other half-wave holds the row's other features
+    float mul;
+    if constexpr (FMT == BS_E4M3) {
+      const int ex = min(max((int)(__float_as_uint(top) >> 23), 1 + 8), 254);
+      mul = __uint_as_float((uint32_t)(254 + 7 - ex) << 23);        // 2^(7 - exponent)
+      back = __uint_as_float((uint32_t)(ex - 7) << 23);
+    } else {
+      top = fmaxf(top, 1.17549435e-38f);
+      mul = 16256.0f / top;
+      back = top * (1.0f / 16256.0f);
+    }
+    if (!(top < __builtin_inff())) back = __uint_as_float(0x7fc00000u);   // an infinite query: no weight is a number
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (float)qb[2 * i + (w >> 1)][4 * (w & 1) + e] * mul;
+        if constexpr (FMT == BS_E4M3) {
+          const uint32_t h = encode4<FMT>(x);
+          float y[4];
+          decode4<FMT>(h, y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = x[e] - y[e];
+          hi[i][w] = (int)h;
+          lo[i][w] = (int)encode4<FMT>(y);
+        } else {
+          uint32_t h = 0, l = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = (int)__builtin_rintf(x[e]), a = (v + 64) >> 7;
+            h |= ((uint32_t)a & 255u) << (8 * e);
+            l |= ((uint32_t)(v - 128 * a) & 255u) << (8 * e);
+          }
+          hi[i][w] = (int)h;
+          lo[i][w] = (int)l;
+        }
+      }
+  }
 };
 
 // ---------------------------------------------------------------- one row tile: waves share the keys out
@@ -430,6 +497,14 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
     issue(QInt<1>{}, u);
   }
 
+  // int8: the queries as integers, 64 VALU instructions a sub-tile less than widening K
+  SplitQueries<FMT, D> sq;
+  float qscale = a.scale_log2e;
+  if constexpr (FMT == BS_I8) {
+    sq.set(qb);
+    qscale *= sq.back;
+  }
+
   // LDS byte offsets of this lane's K and V reads (V rows 16 apart and K rows 32
   // apart have the same swizzle)
   int koff[D / 32], voff[NDT];
@@ -457,23 +532,41 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
       on[sub] = SPT == 1 || (vb + 32 > pad && vb < it.v1);   // wave-uniform
       if (!on[sub]) continue;
       const uint8_t* kt = ring + slot * SLOT + sub * 32 * D;
+      if constexpr (FMT == BS_I8) {
+        i32x4_t x[D / 32];
+        i32x16_t t;
 #pragma unroll
-      for (int rr = 0; rr < 16; ++rr) s[sub][rr] = 0.0f;
+        for (int rr = 0; rr < 16; ++rr) t[rr] = 0;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const v4u x = *reinterpret_cast<const v4u*>(kt + koff[i]);
-        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[0], x[1]), qb[2 * i], s[sub], 0, 0, 0);
-        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[2], x[3]), qb[2 * i + 1], s[sub], 0, 0, 0);
+        for (int i = 0; i < D / 32; ++i) {
+          x[i] = *reinterpret_cast<const i32x4_t*>(kt + koff[i]);
+          t = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], sq.hi[i], t, 0, 0, 0);
+        }
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr) t[rr] <<= 7;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) t = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], sq.lo[i], t, 0, 0, 0);
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr) s[sub][rr] = (float)t[rr];
+      } else {
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr) s[sub][rr] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const v4u x = *reinterpret_cast<const v4u*>(kt + koff[i]);
+          s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[0], x[1]), qb[2 * i], s[sub], 0, 0, 0);
+          s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(x[2], x[3]), qb[2 * i + 1], s[sub], 0, 0, 0);
+        }
       }
       if constexpr (UNI) {
-        f[sub] = uniform(sc[sub * 32]) * a.scale_log2e;
+        f[sub] = uniform(sc[sub * 32]) * qscale;
         vs[sub] = uniform(sc[KT + sub * 32]);
       } else {
 #pragma unroll
         for (int qd = 0; qd < 4; ++qd) {
           const f32x4_t k4 = *reinterpret_cast<const f32x4_t*>(sc + sub * 32 + 8 * qd + 4 * g);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[sub][4 * qd + e] *= k4[e] * a.scale_log2e;
+          for (int e = 0; e < 4; ++e) s[sub][4 * qd + e] *= k4[e];
         }
       }
       if (vb < pad || vb + 32 > nv) {
@@ -503,8 +596,8 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
           col.lsum = fmaf(col.weights(s[sub], f[sub], col.mrun - __builtin_amdgcn_logf(vs[sub])),
                           __builtin_amdgcn_rcpf(vs[sub]), col.lsum);
         } else {
-          col.raise(top16(s[sub]));
-          col.weights_by_key(s[sub], vsk[UNI ? 0 : sub]);
+          col.raise(top16(s[sub]) * qscale);
+          col.weights_by_key(s[sub], qscale, vsk[UNI ? 0 : sub]);
         }
       }
       if (sub == 0) {
@@ -579,72 +672,6 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
 }
 
 // ---------------------------------------------------------------- several row tiles: waves share the ring
-// The queries as numbers of the codes' own kind, so that codes enter the scores' MFMAs
-// as they are: a query is the sum of two of them, which costs two MFMAs of twice the
-// bf16 rate (no more time) and saves the widening of K (32 to 96 VALU instructions a
-// sub-tile).
-//   e4m3: x 2^k = hi + lo, k putting the row's largest element into [128, 256). hi
-//         holds the four leading bits, lo the four that are left of a bf16 number; lo
-//         loses at most 2^-10, which is 2^-17 of the row's largest.
-//   int8: x 16256 / max|x| rounded to an integer (2^-15 of the largest) = 128 hi + lo;
-//         the sums of hi are shifted by 7 before lo's are added. |128 hi + lo| <=
-//         16256, so the sums stay below 128 * 16256 * 128 < 2^29.
-// Lane (g, n) of operand i holds features 32 i + 16 g .. + 15, as a 16-byte read of K
-// finds them; e4m3's MFMAs take operands 2 j and 2 j + 1 together.
-template <int FMT, int D>
-struct SplitQueries {
-  static constexpr int N = D / 32;
-  i32x4_t hi[N], lo[N];
-  float back;              // a score in these units times this is the score
-
-  __device__ void set(const bf16x8_t (&qb)[D / 16]) {
-    float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qb[i][e]));
-    top = max_across<32>(top);             // the other half-wave holds the row's other features
-    float mul;
-    if constexpr (FMT == BS_E4M3) {
-      const int ex = min(max((int)(__float_as_uint(top) >> 23), 1 + 8), 254);
-      mul = __uint_as_float((uint32_t)(254 + 7 - ex) << 23);        // 2^(7 - exponent)
-      back = __uint_as_float((uint32_t)(ex - 7) << 23);
-    } else {
-      top = fmaxf(top, 1.17549435e-38f);
-      mul = 16256.0f / top;
-      back = top * (1.0f / 16256.0f);
-    }
-    if (!(top < __builtin_inff())) back = __uint_as_float(0x7fc00000u);   // an infinite query: no weight is a number
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (float)qb[2 * i + (w >> 1)][4 * (w & 1) + e] * mul;
-        if constexpr (FMT == BS_E4M3) {
-          const uint32_t h = encode4<FMT>(x);
-          float y[4];
-          decode4<FMT>(h, y);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = x[e] - y[e];
-          hi[i][w] = (int)h;
-          lo[i][w] = (int)encode4<FMT>(y);
-        } else {
-          uint32_t h = 0, l = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = (int)__builtin_rintf(x[e]), a = (v + 64) >> 7;
-            h |= ((uint32_t)a & 255u) << (8 * e);
-            l |= ((uint32_t)(v - 128 * a) & 255u) << (8 * e);
-          }
-          hi[i][w] = (int)h;
-          lo[i][w] = (int)l;
-        }
-      }
-  }
-};
-
 // One wave a row tile; up to four waves share the K/V tiles of a 4-stage ring, and two
 // such workgroups a CU (two waves per SIMD). Eight waves in one workgroup a CU, which
 // read each tile once and shared the widening of V, took 67 us instead of 77 for 64
