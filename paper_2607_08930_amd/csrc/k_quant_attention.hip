@@ -139,6 +139,11 @@ __device__ inline void store_block(const QAttnArgs& a, const QPiece& it, int c, 
   }
 }
 
+// An exponent factor that masked scores of -inf can be multiplied by: a product of
+// small factors that fell to zero would turn them into NaN. Scores that this
+// changes are zero either way. A NaN stays one.
+__device__ inline float factor(float x) { return vmax(x, 1.17549435e-38f); }
+
 // a quotient of uniform numbers, which comes out of the vector unit, back in a scalar register
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -504,6 +509,7 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
     sq.set(qb);
     qscale *= sq.back;
   }
+  qscale = factor(qscale);
 
   // LDS byte offsets of this lane's K and V reads (V rows 16 apart and K rows 32
   // apart have the same swizzle)
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
         }
       }
       if constexpr (UNI) {
-        f[sub] = uniform(sc[sub * 32]) * qscale;
+        f[sub] = factor(uniform(sc[sub * 32]) * qscale);
         vs[sub] = uniform(sc[KT + sub * 32]);
       } else {
 #pragma unroll
@@ -842,7 +848,7 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
 
   SplitQueries<FMT, D> sq;
   sq.set(qb);
-  const float qscale = a.scale_log2e * sq.back;
+  const float qscale = factor(a.scale_log2e * sq.back);
   // MFMAs of P V; of the scores (e4m3: 64 features each, twice as long)
   constexpr int NPV = 2 * NDT, NSC = FMT == BS_E4M3 ? D / 32 : D / 16, NSL = NPV + NSC;
   using acc_t = typename std::conditional<FMT == BS_E4M3, f32x16_t, i32x16_t>::type;
@@ -900,7 +906,7 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
 #pragma unroll
       for (int qd = 0; qd < 4; ++qd) k4[qd] = *reinterpret_cast<const f32x4_t*>(scales(s0, H) + 8 * qd + 4 * g);
     }
-    const float f = UNI ? kf * qscale : qscale;
+    const float f = UNI ? factor(kf * qscale) : qscale;
     f32x16_t sc;
     float m3[4], mx = 0.0f, off = 0.0f, ivs = 0.0f, alpha = 1.0f, sum = 0.0f;
     bool resc = false;

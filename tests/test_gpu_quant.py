@@ -282,6 +282,29 @@ def test_attention_group_sizes_far_apart(ctx, fmt):
     say(f"{fmt}: {check_out(w, d):.3f} of the bound")
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("Hq,T,scale", [(2, 32, None), (2, 8, None), (8, 32, None), (8, 8, None), (2, 32, 1e-38), (8, 32, 1e-38)])
+def test_attention_scores_that_vanish(ctx, fmt, Hq, T, scale):
+    """Queries of zero or near nothing against groups of zeros, whose scale is the least there is: every key of
+    the row weighs the same, and the keys of its first and last tiles that do not exist weigh nothing."""
+    torch, _, _ = lazy()
+    rng = np.random.default_rng(31)
+    w = attention_case(rng, [(70, 64, 1), (5, 40, 0), (300, 33, 0)], 32, Hq, 2, 128, T, fmt)
+    for i, r in enumerate(w["reqs"]):
+        t = oracle.geometry(r, 32)
+        w["q"][i, :t.B] = bf16(rng.choice([0.0, 1e-38, -1e-38], size=w["q"][i, :t.B].shape))
+        for c in range(2):
+            for j in range(quant.group_count(r["p"], r["g"], T)):
+                if rng.random() < 0.6:
+                    w["k_scale"][t.row, c, j] = np.float32(2.0 ** -64) / np.float32(quant.QMAX[fmt])
+    w["k8"][:] = np.where(rng.random(w["k8"].shape) < 0.5, 0, w["k8"])
+    d = on_device(w)
+    attend(ctx, w, d, scale=scale or 0.0)
+    torch.cuda.synchronize()
+    # all scores are under 2^-20, so the bound's share for the scores is not used up
+    say(f"{fmt} Hq={Hq} T={T}: {check_out(w, d, scale=scale):.3f} of the bound")
+
+
 def test_attention_reads_only(ctx):
     torch, _, _ = lazy()
     rng = np.random.default_rng(4)
