@@ -111,12 +111,14 @@ struct QItem : QPiece {
 
 constexpr int kQTile = 64;   // virtual keys per planning unit
 constexpr int kQRowTiles = 4;   // most 32-row tiles (waves) per workgroup
+constexpr int kQIssuers = 2;    // waves of it that issue the DMA
 
 struct QAttnArgs {
   const QPiece* far;         // the pieces in device memory, or NULL: in `near`
   QPiece near[kNear];
   int n_pieces, n_split;
   int groups;                // workgroups that share a head's row tiles
+  int spare;                 // waves of the last of them without a row tile or a share of the DMA
   int RTW;                   // row tiles per workgroup
   int KS;                    // RTW = 1: waves that share a row's keys (8, 4 or 2)
   int L, Hq, Hkv, D, G, W, S, lt;

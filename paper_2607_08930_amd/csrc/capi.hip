@@ -1768,6 +1768,7 @@ int bs_quant_cache_block_attention(bs_ctx* c, const bs_req_desc* reqs, int n, in
   a.n_split = meta[1];
   a.parts = static_cast<float*>(ws);
   a.groups = q_rows.groups;
+  a.spare = std::max(0, std::min(q_rows.groups * q_rows.per - q_rows.tiles, q_rows.per - kQIssuers));
   a.RTW = q_rows.per;
   a.KS = meta[3];
   a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.G = Hq / Hkv; a.W = W; a.S = S; a.lt = group_shift(T);

@@ -166,14 +166,10 @@ __device__ inline QItem item_of(const QAttnArgs& a, int b) {
   return it;
 }
 
-// Unit u of the launch's last workgroups: one tensor of one (piece, KV head)
-template <int FMT, int D>
-__device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
-  constexpr int GS = D / 16, RS = 64 / GS, RP = 32 / RS;   // a single row tile: L <= 32
-  if (u >= a.n_pieces * a.Hkv * 2) return;
-  const int tensor = u & 1, i = uniform((u >> 1) / a.Hkv), c = (u >> 1) - i * a.Hkv;
-  const QPiece it = a.piece(i);
-  if (!it.fresh) return;
+// One tensor of a block of up to 32 * TILES rows, read from k_new / v_new
+template <int FMT, int D, int TILES>
+__device__ inline void store_new(const QAttnArgs& a, const QPiece& it, int c, int tensor, int lane) {
+  constexpr int GS = D / 16, RS = 64 / GS, RP = 32 * TILES / RS;
   const uint16_t* src = (tensor ? a.v_new : a.k_new) + ((int64_t)it.req * a.L * a.Hkv + c) * D + (lane % GS) * 16;
   v4u x[RP][2];
 #pragma unroll
@@ -183,6 +179,15 @@ __device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
     x[p][1] = ld16(xp + 8);
   }
   store_block<FMT, D, RP>(a, it, c, tensor, lane, [&](int p, int hh) { return x[p][hh]; });
+}
+
+// Unit u of the launch's last workgroups: one tensor of one (piece, KV head)
+template <int FMT, int D>
+__device__ inline void quantize_block(const QAttnArgs& a, int u, int lane) {
+  if (u >= a.n_pieces * a.Hkv * 2) return;
+  const int tensor = u & 1, i = uniform((u >> 1) / a.Hkv), c = (u >> 1) - i * a.Hkv;
+  const QPiece it = a.piece(i);
+  if (it.fresh) store_new<FMT, D, 1>(a, it, c, tensor, lane);      // a single row tile: L <= 32
 }
 
 // ---------------------------------------------------------------- softmax state of a wave
@@ -684,12 +689,15 @@ __global__ __launch_bounds__(64 * KS, 2) void k_qattn_keys(QAttnArgs a) {
 // Dream-7B rows of equal length, but 57 instead of 52 for ragged ones: a row's two
 // workgroups share their CUs with shorter rows'.
 //
-// What bounds it: instruction issue. A SIMD issues one instruction of its two waves
-// every five cycles or so (a sub-tile is about 150, 12 to 16 of them MFMAs of 32 or 64
-// cycles), and under full load the clock falls from 2.4 to 2.0 GHz.
+// What bounds it: the vector unit, then latencies that two waves a SIMD do not cover. A
+// sub-tile is 104 vector instructions (five cycles each from two waves, an exponential
+// ten; an MFMA hides six of them) beside 510 cycles of MFMAs, and takes 1200 cycles in a lone
+// wave; raises, masks, the queries' split and the output add half as many instructions.
+// A workgroup's start and end take 10 us, and under full load the clock falls from 2.4 to
+// 2.0 GHz.
 template <int FMT, int D, bool UNI>
 __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a) {
-  constexpr int KT = 64, NS = 4, NI = 2;           // keys per stage, stages, waves that issue the DMA
+  constexpr int KT = 64, NS = 4, NI = kQIssuers;   // keys per stage, stages, waves that issue the DMA
   constexpr int NKK = D / 16, NDT = D / 32, NC = D / 16, NCB = D / 8;
   constexpr int TILE = KT * D, STAGE = 2 * TILE;   // bytes: K tile, then V tile
   constexpr int RPB = 1024 / D;                    // rows per 1 KiB DMA block
@@ -708,6 +716,25 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
   const bool issuer = w < NI;
   const int seam_ = keys.seam;
   const int r = (it.rt0 + w) * 32 + n;
+  const int nsub = v1 > v0 ? (v1 - v0 + 31) / 32 : 0;
+  // The last of a head's workgroups may have waves to spare (a.spare of them, without a row
+  // and without a share of the DMA): they keep step with the others, then write the block
+  // into the cache, which otherwise the first workgroup's last waves do before their
+  // first tiles (64 Dream-7B requests, seven row tiles a head, of one length: 55 us
+  // instead of 59; ragged: 49.7 instead of 50.6).
+  if (it.rt0 + a.RTW == a.groups * a.RTW && w >= a.RTW - a.spare) {
+    const int steps = (it.fresh ? 2 : 0) + (nsub > 0 ? 1 + nsub / 2 : 0);
+    for (int i = 0; i < steps; ++i) __builtin_amdgcn_s_barrier();
+    if (a.write_back && it.fresh)
+      for (int tensor = w - (a.RTW - a.spare); tensor < 2; tensor += a.spare) {
+        if (a.L > 32)
+          store_new<FMT, D, 2>(a, it, it.kvh, tensor, lane);
+        else
+          store_new<FMT, D, 1>(a, it, it.kvh, tensor, lane);
+      }
+    if (it.part < 0) __builtin_amdgcn_s_barrier();     // ahead of the staged rows
+    return;
+  }
 
   bf16x8_t qb[NKK];
   load_queries<D>(a, it, r, g, qb);
@@ -806,7 +833,7 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
     // K and V by the last two waves: where there are enough, those that issue no DMA, so
     // that no stage waits for the stores
     const int wt = w - (a.RTW - 2);
-    if (a.write_back && it.rt0 == 0 && (wt == 0 || wt == 1)) {
+    if (a.write_back && a.spare == 0 && it.rt0 == 0 && (wt == 0 || wt == 1)) {
       constexpr int GS = D / 16, RS = 64 / GS;
       auto row = [&](int p, int hh) {
         const int x = p * RS + lane / GS, ch = 2 * (lane % GS) + hh;
@@ -852,7 +879,6 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
   // MFMAs of P V; of the scores (e4m3: 64 features each, twice as long)
   constexpr int NPV = 2 * NDT, NSC = FMT == BS_E4M3 ? D / 32 : D / 16, NSL = NPV + NSC;
   using acc_t = typename std::conditional<FMT == BS_E4M3, f32x16_t, i32x16_t>::type;
-  const int nsub = v1 > v0 ? (v1 - v0 + 31) / 32 : 0;
   const int u0 = v0 + 32 <= pad ? 1 : 0;             // a first sub-tile without keys
   acc_t sA, sB;
   i32x4_t rk[D / 32];                                // K codes of a sub-tile
@@ -995,8 +1021,9 @@ __global__ __launch_bounds__(64 * kQRowTiles, 2) void k_qattn_group(QAttnArgs a)
         const i32x2_t& x = rv[i + 1 == NSL ? 0 : (i + 1) & 3];
         fr[i + 1 == NSL ? 0 : (i + 1) & 1] = widen8<FMT>((uint32_t)x[0], (uint32_t)x[1]);
       }
-      // the softmax: steps 0 .. 7 beside P V, 8 .. 15 beside the scores
-      const int b0 = i < NPV ? i * 8 / NPV : 8 + (i - NPV) * 8 / NSC, b1 = i < NPV ? (i + 1) * 8 / NPV : 8 + (i + 1 - NPV) * 8 / NSC;
+      // the softmax: steps 0 .. 3 beside P V, which has V's widening, 4 .. 15 beside the
+      // scores (half and half: 1 us of 50 more for 64 Dream-7B requests)
+      const int b0 = i < NPV ? i * 4 / NPV : 4 + (i - NPV) * 12 / NSC, b1 = i < NPV ? (i + 1) * 4 / NPV : 4 + (i + 1 - NPV) * 12 / NSC;
 #pragma unroll
       for (int st = b0; st < b1; ++st)
         step(st);
