@@ -57,9 +57,9 @@ class QuantCache:
                                        self.R, self.W, write_back, out, ws, ws_bytes, stream=stream)
 
     def admit(self, ctx: Context, segs: np.ndarray, p, g, stg_k, stg_v) -> None:
-        """On the current stream: quantises staged rows and moves them in. stg_k, stg_v: bf16 [layers][n][Hkv][Ws][D], row a holding a
-        request of prompt length p[a] and generation length g[a] from column 0; ``segs`` (SEG_DTYPE) says where
-        the staged rows go, as for a bf16 cache."""
+        """Quantises staged rows and moves them in, on the current stream. stg_k, stg_v: bf16
+        [layers][n][Hkv][Ws][D], row a holding a request of prompt length p[a] and generation length g[a]
+        from column 0; ``segs`` (SEG_DTYPE) says where the staged rows go, as for a bf16 cache."""
         n, Ws = stg_k.shape[1], stg_k.shape[3]
         stg = QuantCache(self.layers, n, Ws, self.Hkv, self.D, self.L, self.name, self.T, self.k.device, empty=True)
         reqs = np.zeros(n, REQ_DTYPE)
@@ -68,29 +68,34 @@ class QuantCache:
             stg.write(ctx, reqs, l, stg_k[l], stg_v[l])
         self.move(ctx, segs, None, stg)
 
-    def move(self, ctx: Context, segs: np.ndarray, src: QuantCache | None, stg: QuantCache | None = None,
-             stream=None) -> None:
-        """Whole rows from the caches ``src`` (src_kind 0) and ``stg`` (src_kind 1) into this one, every layer:
-        codes as pairs of bytes, scale rows as they are (a row that only changes its column keeps its scales)."""
+    def move(self, ctx: Context, segs: np.ndarray, src: QuantCache | None, stg: QuantCache | None = None) -> None:
+        """Whole rows, one segment each, from the caches ``src`` (src_kind 0, which may be this one) and ``stg``
+        (src_kind 1) into this one, every layer, on the current stream: codes as pairs of bytes, scale rows as
+        they are (groups belong to the row, not to its column)."""
         for c in (src, stg):
             if c is not None and (c.layers, c.Hkv, c.D, c.fmt, c.T) != (self.layers, self.Hkv, self.D, self.fmt, self.T):
                 raise ValueError("rows move between caches of the same layers, heads, format and groups")
-
-        def box(c, scales):
-            if c is None:
-                return None, None, 0, 1, 1
-            a, b = (c.k_scale, c.v_scale) if scales else (c.k, c.v)
-            return a, b, a[0].numel() * a.element_size(), c.R, c.S // 4 if scales else c.W
-
-        bs_kv_scatter_compact(ctx, segs, self.layers, self.Hkv, self.D // 2, BS_BF16, *box(src, False), *box(stg, False),
-                              *box(self, False), stream=stream)
-        rows = np.array(segs, copy=True)
+        segs = np.asarray(segs)
+        rows = segs.copy()
         rows["src_col"] = rows["dst_col"] = 0
         for kind, c in ((0, src), (1, stg)):
             if c is not None:
-                rows["len"][rows["src_kind"] == kind] = min(c.S, self.S) // 4
-        rows["len"][segs["len"] == 0] = 0
-        if src is self:
-            rows = rows[(rows["src_kind"] != 0) | (rows["src_row"] != rows["dst_row"])]
-        bs_kv_scatter_compact(ctx, rows, self.layers, self.Hkv, 4, BS_F32, *box(src, True), *box(stg, True),
-                              *box(self, True), stream=stream)
+                rows["len"][(rows["src_kind"] == kind) & (rows["len"] > 0)] = min(c.S, self.S) // 4
+        live = rows["dst_row"][rows["len"] > 0]
+        if len(np.unique(live)) != len(live):
+            raise ValueError("two segments for one row: rows move whole")
+
+        def box(c, k, v, width):
+            return (None, None, 0, 1, 1) if c is None else (k, v, k[0].numel() * k.element_size(), c.R, width)
+
+        def codes(c):
+            return box(c, *((c.k, c.v, c.W) if c is not None else (None, None, 0)))
+
+        def scales(c, copied=False):
+            if c is None:
+                return box(None, None, None, 0)
+            # rows of one box may change places without their cells meeting, but their scales always start at 0
+            return box(c, *((x.clone() if copied else x) for x in (c.k_scale, c.v_scale)), c.S // 4)
+
+        bs_kv_scatter_compact(ctx, segs, self.layers, self.Hkv, self.D // 2, BS_BF16, *codes(src), *codes(stg), *codes(self))
+        bs_kv_scatter_compact(ctx, rows, self.layers, self.Hkv, 4, BS_F32, *scales(src, src is self), *scales(stg), *scales(self))

@@ -200,5 +200,20 @@ def test_rows_move_between_caches(fmt):
         for l in range(2):
             for x, y in zip(read(b, there, l), before[l]):
                 assert all(torch.equal(p, q) for p, q in zip(x, y))
+        # two rows change places inside a box, at columns where their cells do not meet
+        c = QuantCache(2, 2, 300, kv, D, blk, fmt, T)
+        pair = moved[:2].copy()
+        pair["row"], pair["off"] = [0, 1], [0, 60]
+        c.move(ctx, np.array([(0, m["row"], m["off"], t["row"], t["off"], m["p"] + m["g"]) for m, t in zip(moved, pair)],
+                             bs.SEG_DTYPE), a)
+        swapped = pair.copy()
+        swapped["row"], swapped["off"] = [1, 0], [200, 200]
+        c.move(ctx, np.array([(0, m["row"], m["off"], t["row"], t["off"], m["p"] + m["g"]) for m, t in zip(pair, swapped)],
+                             bs.SEG_DTYPE), c)
+        for l in range(2):
+            for x, y in zip(read(c, swapped, l), before[l]):
+                assert all(torch.equal(p, q) for p, q in zip(x, y[:2]))
+        with pytest.raises(ValueError, match="rows move whole"):
+            c.move(ctx, np.array([(0, 0, 0, 1, 0, 10), (0, 1, 0, 1, 20, 10)], bs.SEG_DTYPE), a)
         with pytest.raises(ValueError, match="same layers"):
             QuantCache(2, 4, 50, kv, D, blk, fmt, 16).move(ctx, np.zeros(0, bs.SEG_DTYPE), a)
