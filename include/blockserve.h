@@ -400,11 +400,11 @@ int bs_kv_dequantize(bs_ctx* ctx, const bs_req_desc* reqs, int n, int L, int R, 
  * block's cells and scales, exactly as bs_kv_quantize would from a box; the
  * cache is otherwise only read, and padding and the stale block slot never are
  * (their scales neither). Sums and softmax statistics are fp32, weights are
- * rounded to bf16. Up to 32 query rows a KV head (L * Hq / Hkv), products of
- * queries and codes are exact. Beyond, a query element meets the codes as a number
- * of theirs plus another: off by at most 2^-17 (BS_E4M3) or 2^-15 (BS_I8) of the
- * largest element of its row and head, which is less than the input's own rounding
- * of that element. The block's own keys always meet the queries as given.
+ * rounded to bf16. With BS_E4M3 and up to 32 query rows a KV head (L * Hq / Hkv),
+ * products of queries and codes are exact. Otherwise a query element meets the codes
+ * as the sum of two numbers of their kind: off by at most 2^-17 (BS_E4M3) or 2^-15
+ * (BS_I8) of the largest element of its row and head, which is less than the input's
+ * own rounding of that element. The block's own keys always meet the queries as given.
  * Scales must be positive and finite, within 2^-80 .. 2^80.
  * Supported: D in {64, 128}, L <= 64, Hq / Hkv <= 8, T a divisor of L,
  * n * Hkv <= 2^20, W * D < 2^31; tensors 16-byte aligned (scales 4), ws too.

@@ -17,10 +17,11 @@
 //
 // Per sub-tile: S^T = K Q^T with v_mfma_f32_32x32x16_bf16 (keys on the M axis),
 // online softmax on one query column a lane, O^T += V^T P^T with the weights fed
-// straight from the accumulators. Codes become bf16 in registers, exactly (e4m3
-// has 4 significant bits, int8 7, bf16 8); a K read of 16 codes feeds two MFMAs,
-// since the order of the contraction is free, and V comes out of LDS transposed,
-// 8 keys of one feature a lane (ds_read_b64_tr_b8). The K scale is folded into the
+// straight from the accumulators. V's codes, and K's of e4m3 with one row tile, become
+// bf16 in registers, exactly (e4m3 has 4 significant bits, int8 7, bf16 8); a K read of
+// 16 codes feeds two MFMAs, since the order of the contraction is free, and V comes out
+// of LDS transposed, 8 keys of one feature a lane (ds_read_b64_tr_b8). Elsewhere K's
+// codes meet the queries as they are (SplitQueries). The K scale is folded into the
 // exponent's factor and the V scale into its offset:
 //   p' = vs 2^(s ks c - m) = 2^(s ks c - (m - log2 vs)),
 // so neither costs an instruction per key; the row sum takes (sum p') / vs.

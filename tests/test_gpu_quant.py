@@ -9,8 +9,8 @@ the output to 2^-8 of its value, so |d| <= 2^-8 |out| + (2^-8 + 2^-9) spread wit
 the spread of oracle.quant; 2^-9 covers the scores: their error e moves a weight by
 the factor exp(e). Of it, e <= 128 * 2^-24 * sum |q k| from the fp32 sums stays under
 2^-10 for the sum |q k| scale <= 128 that the inputs keep, as does the hardware
-exp2. With more than 32 query rows a KV head a query element is off by up to 2^-17
-(e4m3) or 2^-15 (int8) of its row's largest, with either sign: over a key of
+exp2. A query element is off by up to 2^-15 (int8) or, with more than 32 query rows a
+KV head, 2^-17 (e4m3) of its row's largest, with either sign: over a key of
 deviation s that is a score error of deviation 2^-15 max|q| s / sqrt(3), 2^-14 s for
 the normal queries here, and it averages out over the keys of a row.
 Norm: fp32 sums of 256 squares at most, one reciprocal square root and two
@@ -515,6 +515,42 @@ def test_captured_by_a_context_that_never_ran():
                     num = quant.row_numbers(r, c, d["v8"].cpu().numpy(), d["v_scale"].cpu().numpy(), 32, "e4m3")
                     got = box[1][t.row, c, t.off:t.off + len(num)].float().cpu().numpy()
                     assert (np.abs(got - num) <= 2.0 ** -8 * np.abs(num)).all()
+
+
+def test_long_lists_captured_and_replayed(ctx):
+    # 80 requests: uploaded by the call before, whose slot then keeps them whatever else is uploaded
+    torch, bs, _ = lazy()
+    rng = np.random.default_rng(18)
+    w = attention_case(rng, [(int(rng.integers(0, 90)), int(rng.integers(1, 40)), 0) for _ in range(80)], 8, 4, 2, 64, 8, "e4m3")
+    d = on_device(w)
+    box = [torch.zeros((w["R"], 2, w["W"], 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    qo, ko = torch.empty_like(d["q"]), torch.empty_like(d["k_new"])
+
+    def calls():
+        bs.bs_qk_norm_rope(ctx, w["reqs"], 8, w["R"], w["W"], False, 4, 2, 64, bs.BS_BF16, d["q"], 256, d["k_new"], 128, None,
+                           None, 1e-6, 1e4, qo, ko)
+        bs.bs_quant_cache_block_attention(ctx, w["reqs"], 8, 4, 2, 64, 0, 8, 0.0, qo, ko, d["v_new"], d["k8"], d["v8"],
+                                          d["k_scale"], d["v_scale"], w["S"], w["R"], w["W"], True, d["out"])
+        bs.bs_kv_dequantize(ctx, w["reqs"], 8, w["R"], w["W"], 2, 64, bs.BS_BF16, 0, 8, d["k8"], d["v8"], d["k_scale"],
+                            d["v_scale"], w["S"], *box)
+
+    calls()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (d["out"], *box, d["k8"], d["k_scale"])]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for rep in range(3):
+        for x in (d["out"], *box):
+            x.zero_()
+        for i in range(24):                        # enough other lists to turn the upload slots over
+            other = np.roll(w["reqs"], i + 1)
+            bs.bs_kv_dequantize(ctx, other, 8, w["R"], w["W"], 2, 64, bs.BS_BF16, 0, 8, d["k8"], d["v8"], d["k_scale"],
+                                d["v_scale"], w["S"], torch.empty_like(box[0]), torch.empty_like(box[0]))
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((d["out"], *box, d["k8"], d["k_scale"]), want):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), f"replay {rep}"
 
 
 @pytest.mark.parametrize("n", [64, 65, 130])
