@@ -143,6 +143,8 @@ class BlockServeError(RuntimeError):
 
 
 def _ptr(x):
+    if type(x) is torch.Tensor:      # most arguments
+        return x.data_ptr()
     if x is None:
         return None
     if isinstance(x, int):
